@@ -242,17 +242,17 @@ def prepare(case, seed):
     elif kind == "act8":
         s["out"] = torch.zeros_like(d["A"])
         if own:
-            s["packed"] = torch.zeros((n, m, nb.act8_bytes(case["tokens"], case["dim"])),
+            s["packed"] = torch.zeros((n, m, nb.act_bytes(case["tokens"], case["dim"])),
                                       dtype=torch.uint8, device=DEV)
     else:
         # the layer's input is gone by now; what was kept of it is its 8-bit form
         A = d.pop("A")
         s["G"] = torch.zeros((n, m, _row(case["dim"] * case["out"])), device=DEV)
         if own:
-            s["packed"] = torch.zeros((n, m, nb.act8_bytes(case["tokens"], case["dim"])),
+            s["packed"] = torch.zeros((n, m, nb.act_bytes(case["tokens"], case["dim"])),
                                       dtype=torch.uint8, device=DEV)
-            nb.act8_pack(A, s["mask"], s["packed"])
-            s["ws"] = workspace(nb.act8_workspace_bytes(n, m, case["tokens"], case["dim"], case["out"]))
+            nb.act_pack(A, s["mask"], s["packed"])
+            s["ws"] = workspace(nb.act_workspace_bytes(n, m, case["tokens"], case["dim"], case["out"]))
         else:
             q, step = zip(*(_quantise(A[i, j]) for i in range(n) for j in range(m)))
             s["q"], s["step"] = torch.stack(q), torch.stack(step)
@@ -285,10 +285,10 @@ def _run_own(s):
                      lengths=d["lengths"] if c["ragged"] else None)
         return [s["dx"], s["dg"], s["dh0"], s["G"]]
     if kind == "act8":
-        nb.act8_pack(d["A"], mask, s["packed"])
-        nb.act8_unpack(s["packed"], mask, s["out"])
+        nb.act_pack(d["A"], mask, s["packed"])
+        nb.act_unpack(s["packed"], mask, s["out"])
         return s["out"]
-    nb.act8_grad(s["packed"], d["dY"], mask, s["G"], OFFSET, c["dim"], s["ws"])
+    nb.act_grad(s["packed"], d["dY"], mask, s["G"], OFFSET, c["dim"], s["ws"])
     return s["G"]
 
 
