@@ -418,6 +418,148 @@ nbsgd_status nbsgd_mlp_loss(const float *params, const nbsgd_mlp_shape *s, const
                             int32_t count, float *losses, void *workspace, size_t workspace_bytes,
                             void *stream);
 
+/* ------------------------------------------------------- token models
+ * Gradient calls for the parts of a recurrent language model, beside
+ * nbsgd_mlp_grad and with its conventions: learner i's parameters are read
+ * from its row of X, the gradient of mini-batch (i, j) is written into row
+ * (i, j) of G, and the mini-batches with mask[i*m+j] == 0 are neither read
+ * nor written.  A mini-batch's results depend on its own data and replica
+ * alone, bit for bit: not on which or how many other mini-batches the call
+ * has.
+ *
+ * Parameters and their gradients are fp32.  `ld` is the distance in floats
+ * between the rows of X (and of G); the pointers passed are those of the
+ * operator's own parameters in row 0 (row base + offset), 16-byte aligned,
+ * and ld is a multiple of 4 and at least their number (NBSGD_E_SHAPE).
+ * Activations are `dtype` rows, one row a token, with the rows of a call
+ * ld* elements apart in the order mini-batch, (sequence,) token; they need
+ * the alignment of their element only, and a row's elements past its width
+ * are never touched.  Every sum, softmax-like gate and state is held in fp32;
+ * a bf16 result is rounded once, to nearest even.
+ * Tokens and lengths are device int32, contiguous.  The device pointers of
+ * outputs must not overlap those of inputs or each other (NBSGD_E_ARG), except
+ * where a call says so.  `stream` must belong to the current device
+ * (NBSGD_E_ARG).  Workspaces are device memory, 16-byte aligned, for one call
+ * at a time: calls that may overlap, and captured graphs that may run at the
+ * same time, need their own.  The kernels write every byte of a workspace that
+ * they read, clear nothing with a memset and may be captured into a graph
+ * (mask and scalars are then those of the capture).
+ * A mask without a finished mini-batch is valid; nothing is enqueued then. */
+typedef enum { NBSGD_F32 = 0, NBSGD_BF16 = 1 } nbsgd_dtype;
+
+#define NBSGD_MAX_TOKENS 262144      /* tokens of a mini-batch: embeddings, 8-bit activations */
+#define NBSGD_MAX_LENGTH 16777216    /* tokens of a sequence of the recurrence */
+#define NBSGD_MAX_VOCAB 16777216
+#define NBSGD_MAX_WIDTH 65536        /* elements of an activation row */
+
+/* Embedding lookup with scaling:
+ *   Y[i][j][t][:] = scale * E_i[tokens[i][j][t]][:]
+ * and zeros where the token lies outside [0, vocab) (padding).
+ * E       device fp32, learner i's table [vocab][dim] at E + i*ld
+ * tokens  [n][m][T], T >= 0
+ * Y       [n][m][T] rows of dim elements, ldy >= dim apart
+ * Errors: NBSGD_E_ARG, NBSGD_E_SHAPE, NBSGD_E_ALIGN, NBSGD_E_UNSUPPORTED,
+ *         NBSGD_E_HIP; the same for every call of this section.           */
+nbsgd_status nbsgd_embed(const float *E, int64_t ld, int32_t n, int32_t m, int32_t vocab,
+                         int32_t dim, float scale, const int32_t *tokens, int32_t T,
+                         const uint8_t *mask, void *Y, int64_t ldy, int32_t dtype, void *stream);
+
+/* Gradient of the lookup, every row of the table written:
+ *   G[i][j][v][:] = scale * sum_{t : tokens[i][j][t] == v} dY[i][j][t][:]
+ * The tokens are sorted first, so that a row's sum runs over its own tokens in
+ * their order and needs no atomics.  Rows of dY whose token lies outside
+ * [0, vocab) are not read.
+ * G  device fp32, the gradient of mini-batch (i, j) at G + (i*m + j)*ld
+ * workspace  nbsgd_embed_workspace_bytes(n, m, T, vocab, dim)             */
+nbsgd_status nbsgd_embed_workspace_bytes(int32_t n, int32_t m, int32_t T, int32_t vocab,
+                                         int32_t dim, size_t *bytes);
+nbsgd_status nbsgd_embed_grad(const void *dY, int64_t ldy, int32_t dtype, int32_t n, int32_t m,
+                              int32_t T, const int32_t *tokens, int32_t vocab, int32_t dim,
+                              float scale, const uint8_t *mask, float *G, int64_t ld,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gated linear recurrence over the tokens of each sequence, one state a
+ * channel:
+ *   a_t = 1 / (1 + exp(-(g_t + bias)))     h_t = a_t h_{t-1} + (1 - a_t) x_t
+ * h_0 is the given first state or zero.  T = 1 with h0 and h_last is the form
+ * that serves one token at a time; h_last may be h0 itself.
+ * x, g     [n][m][batch][T] rows of dim elements, both ldx >= dim apart (they
+ *          may be the two halves of one buffer's rows)
+ * bias     device fp32 [dim] at bias + i*ld for learner i, or NULL (zero; ld
+ *          is ignored)
+ * lengths  [n][m][batch], or NULL: every sequence has T tokens.  Values are
+ *          clamped into [0, T].  Past its length a sequence's x and g are not
+ *          read, h is 0 and the state stays as it is.
+ * h0       device fp32 [n][m][batch][dim], or NULL: zero
+ * h        [n][m][batch][T] rows, ldh >= dim apart
+ * h_last   device fp32 [n][m][batch][dim], or NULL: the state after the last
+ *          token
+ * states   device fp32 [n][m][batch][ceil(T / NBSGD_SCAN_INTERVAL)][dim], or
+ *          NULL: the state before token 0, 256, 512, ...; what the backward
+ *          pass needs besides x and g (h itself is not kept for it)
+ * workspace  nbsgd_scan_workspace_bytes, for nbsgd_scan and nbsgd_scan_grad
+ * n*m*batch*ceil(dim/64) is at most 2^22 (NBSGD_E_UNSUPPORTED).           */
+#define NBSGD_SCAN_INTERVAL 256
+nbsgd_status nbsgd_scan_workspace_bytes(int32_t n, int32_t m, int32_t batch, int32_t T,
+                                        int32_t dim, size_t *bytes);
+nbsgd_status nbsgd_scan(const void *x, const void *g, int64_t ldx, int32_t dtype, int32_t n,
+                        int32_t m, int32_t batch, int32_t T, int32_t dim, const float *bias,
+                        int64_t ld, const int32_t *lengths, const uint8_t *mask, const float *h0,
+                        void *h, int64_t ldh, float *h_last, float *states, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/* Backward pass of nbsgd_scan: with l_t the gradient of the loss with respect
+ * to h_t through every later token,
+ *   l_t = dh_t + a_{t+1} l_{t+1}   (from dh_last after the last token)
+ *   dx_t = l_t (1 - a_t)           dg_t = l_t (h_{t-1} - x_t) a_t (1 - a_t)
+ *   dh0 = a_1 l_1                  Gbias = sum over the mini-batch's tokens of dg_t
+ * x, g, bias, lengths, mask  as in the forward call; states its output
+ * dh       [n][m][batch][T] rows, lddh >= dim apart; not read past a length
+ * dh_last  device fp32 [n][m][batch][dim], or NULL: zero
+ * dx, dg   rows ldx apart, laid out as x and g; zeros past a length
+ * dh0      device fp32 [n][m][batch][dim], or NULL; may be dh_last itself
+ * Gbias    device fp32 [dim] at Gbias + (i*m + j)*ld, or NULL               */
+nbsgd_status nbsgd_scan_grad(const void *x, const void *g, int64_t ldx, int32_t dtype, int32_t n,
+                             int32_t m, int32_t batch, int32_t T, int32_t dim, const float *bias,
+                             int64_t ld, const int32_t *lengths, const uint8_t *mask,
+                             const float *states, const void *dh, int64_t lddh,
+                             const float *dh_last, void *dx, void *dg, float *dh0, float *Gbias,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/* Activations kept for the backward pass in 8 bits.  32 consecutive tokens of
+ * a channel share a step 2^k, the smallest with |rne(A / 2^k)| <= 127 for all
+ * of them, k in [-126, 121] (at 121 larger quotients are clamped to +-127), and
+ * each keeps the whole number q = rne(A / 2^k): off by at most half a step.  A
+ * block that holds an infinity or a NaN stands for NaNs.
+ * A       [n][m][T] rows of dim elements, lda >= dim apart
+ * packed  device, mini-batch (i, j) at packed + (i*m + j) * bytes, bytes as
+ *         nbsgd_act_bytes gives them (a multiple of 16): for every block of 32
+ *         tokens and channel 32 int8 (zeros past T), block-major; then for every
+ *         four blocks and channel four bytes k + 127 (255: NaNs; 0 past the last
+ *         block).  16-byte aligned.
+ * nbsgd_act_unpack writes the values q * 2^k, rounded to dtype (bf16 holds them
+ * exactly).                                                               */
+nbsgd_status nbsgd_act_bytes(int32_t T, int32_t dim, int64_t *bytes);
+nbsgd_status nbsgd_act_pack(const void *A, int64_t lda, int32_t dtype, int32_t n, int32_t m,
+                             int32_t T, int32_t dim, const uint8_t *mask, void *packed,
+                             void *stream);
+nbsgd_status nbsgd_act_unpack(const void *packed, int32_t n, int32_t m, int32_t T, int32_t dim,
+                               const uint8_t *mask, void *A, int64_t lda, int32_t dtype,
+                               void *stream);
+
+/* Weight gradient of a layer Y = A W from the packed activations:
+ *   G[i][j][k][c] = sum_t (q 2^k)[i][j][t][k] dY[i][j][t][c]
+ * on the matrix cores, the products exact and their sums in fp32 (q 2^k has 7
+ * significant bits and dY 8, so both are bf16 as they are).
+ * dY  bf16 [n][m][T] rows of `out` elements, ldy >= out apart
+ * G   device fp32, W's gradient [dim][out] row-major at G + (i*m + j)*ld
+ * workspace  nbsgd_act_workspace_bytes(n, m, T, dim, out)                */
+nbsgd_status nbsgd_act_workspace_bytes(int32_t n, int32_t m, int32_t T, int32_t dim, int32_t out,
+                                        size_t *bytes);
+nbsgd_status nbsgd_act_grad(const void *packed, const void *dY, int64_t ldy, int32_t n, int32_t m,
+                             int32_t T, int32_t dim, int32_t out, const uint8_t *mask, float *G,
+                             int64_t ld, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------- errors
  * Text of the last failed check or HIP error on the calling thread ("" if
  * none).  The pointer stays valid until the next nbsgd call on the thread. */

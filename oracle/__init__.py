@@ -24,6 +24,9 @@ sum).  Modules:
 * ``mlp``      - the end-to-end two-layer MLP workload: forward/backward
                  per mini-batch, local shuffling (Alg. 1 initialisation),
                  training under any mixing kind.
+* ``tokens``   - the token models' operators: embeddings, the gated
+                 recurrence, 8-bit activations, each with its gradient and the
+                 bound of a 32-bit computation's error.
 * ``workload`` - drivers: a workload description mapped to the oracle's delay
                  model, mixing matrices and order; column windows of the
                  seeded inputs; several iterations of the step.
@@ -32,4 +35,4 @@ Parity pins for each function live in ``tests/test_oracle_*.py``; functions
 with no pin say "parity unpinned" in their docstring.
 """
 
-from . import mixing, mlp, philox, schedule, step, workload  # noqa: F401
+from . import mixing, mlp, philox, schedule, step, tokens, workload  # noqa: F401

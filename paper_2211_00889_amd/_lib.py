@@ -22,6 +22,8 @@ MIX_THEN_STEP, STEP_THEN_MIX = 0, 1
 DELAY_CONST, DELAY_EXP, DELAY_LOMAX = 0, 1, 2
 MAX_LEARNERS, MAX_MINIBATCHES = 16, 64
 SLOW_NONE, SLOW_RANDOM = -1, -2
+F32, BF16 = 0, 1
+SCAN_INTERVAL = 256
 
 EXPORTS = ("nbsgd_sample_mask", "nbsgd_iteration_accounting", "nbsgd_accumulate", "nbsgd_mix", "nbsgd_update", "nbsgd_step",
            "nbsgd_step_strided", "nbsgd_step_server", "nbsgd_row_stride",
@@ -30,6 +32,10 @@ EXPORTS = ("nbsgd_sample_mask", "nbsgd_iteration_accounting", "nbsgd_accumulate"
            "nbsgd_matcha_destroy", "nbsgd_mlp_param_count",
            "nbsgd_mlp_workspace_bytes", "nbsgd_minibatch_indices", "nbsgd_mlp_grad",
            "nbsgd_mlp_grad_strided", "nbsgd_mlp_grad_noalloc", "nbsgd_mlp_loss",
+           "nbsgd_embed", "nbsgd_embed_workspace_bytes", "nbsgd_embed_grad",
+           "nbsgd_scan_workspace_bytes", "nbsgd_scan", "nbsgd_scan_grad",
+           "nbsgd_act_bytes", "nbsgd_act_pack", "nbsgd_act_unpack",
+           "nbsgd_act_workspace_bytes", "nbsgd_act_grad",
            "nbsgd_last_error")
 
 
@@ -104,6 +110,27 @@ def load():
                                    _c_void_p],
         "nbsgd_mlp_loss": [_c_void_p, ctypes.POINTER(MlpShape), _c_void_p, _c_void_p, _i64, _c_void_p,
                            _i32, _c_void_p, _c_void_p, ctypes.c_size_t, _c_void_p],
+        "nbsgd_embed": [_c_void_p, _i64, _i32, _i32, _i32, _i32, _f32, _c_void_p, _i32, _c_void_p,
+                        _c_void_p, _i64, _i32, _c_void_p],
+        "nbsgd_embed_workspace_bytes": [_i32, _i32, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_size_t)],
+        "nbsgd_embed_grad": [_c_void_p, _i64, _i32, _i32, _i32, _i32, _c_void_p, _i32, _i32, _f32,
+                             _c_void_p, _c_void_p, _i64, _c_void_p, ctypes.c_size_t, _c_void_p],
+        "nbsgd_scan_workspace_bytes": [_i32, _i32, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_size_t)],
+        "nbsgd_scan": [_c_void_p, _c_void_p, _i64, _i32, _i32, _i32, _i32, _i32, _i32, _c_void_p, _i64,
+                       _c_void_p, _c_void_p, _c_void_p, _c_void_p, _i64, _c_void_p, _c_void_p,
+                       _c_void_p, ctypes.c_size_t, _c_void_p],
+        "nbsgd_scan_grad": [_c_void_p, _c_void_p, _i64, _i32, _i32, _i32, _i32, _i32, _i32, _c_void_p,
+                            _i64, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _i64, _c_void_p,
+                            _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, ctypes.c_size_t,
+                            _c_void_p],
+        "nbsgd_act_bytes": [_i32, _i32, ctypes.POINTER(_i64)],
+        "nbsgd_act_pack": [_c_void_p, _i64, _i32, _i32, _i32, _i32, _i32, _c_void_p, _c_void_p,
+                            _c_void_p],
+        "nbsgd_act_unpack": [_c_void_p, _i32, _i32, _i32, _i32, _c_void_p, _c_void_p, _i64, _i32,
+                              _c_void_p],
+        "nbsgd_act_workspace_bytes": [_i32, _i32, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_size_t)],
+        "nbsgd_act_grad": [_c_void_p, _c_void_p, _i64, _i32, _i32, _i32, _i32, _i32, _c_void_p,
+                            _c_void_p, _i64, _c_void_p, ctypes.c_size_t, _c_void_p],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -435,3 +462,233 @@ def mlp_loss(params, dims, data, labels, idx, losses, workspace, stream=None):
     _check(load().nbsgd_mlp_loss(_dev(params, "params"), ctypes.byref(_shape(*dims)), _dev(data, "data"),
                                  _i32_dev(labels, "labels"), data.shape[0], idx.tobytes(), idx.size,
                                  _dev(losses, "losses"), ws, ws_bytes, _stream(params, stream)))
+
+
+# ------------------------------------------------------------ token models
+def _rows(t, name, lead, width=None, like=None):
+    """(pointer, row stride, dtype) of activations [*lead, width]: float32 or bfloat16 rows, a
+    constant number of elements apart in the order of the leading dimensions."""
+    torch = _torch or _use_torch()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    dtype = F32 if t.dtype == torch.float32 else BF16 if t.dtype == torch.bfloat16 else None
+    if dtype is None or (like is not None and t.dtype != like.dtype):
+        raise TypeError(f"{name} must be float32 or bfloat16" + (", as the other rows" if like is not None else ""))
+    if t.dim() != len(lead) + 1 or tuple(t.shape[:-1]) != lead or (width is not None and t.shape[-1] != width):
+        raise ValueError(f"{name} must be {list(lead) + [width if width is not None else 'width']}")
+    shape, strides = t.shape, t.stride()
+    if shape[-1] > 1 and strides[-1] != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    if not t.numel():
+        return t.data_ptr(), shape[-1], dtype
+    ld = rows = None
+    for k in range(len(lead) - 1, -1, -1):  # dimensions of one entry have no stride of their own
+        if shape[k] != 1:
+            if ld is None:
+                ld, rows = strides[k], shape[k]
+            elif strides[k] != ld * rows:
+                raise ValueError(f"{name}: the rows must lie a constant stride apart")
+            else:
+                rows *= shape[k]
+    return t.data_ptr(), shape[-1] if ld is None else ld, dtype
+
+
+def _whole(t, name, dtype, shape):
+    """Pointer of a contiguous device tensor of this type and shape; None stays null."""
+    if t is None:
+        return None
+    torch = _torch or _use_torch()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}")
+    return t.data_ptr()
+
+
+def _params(t, name, lead, offset, count):
+    """(pointer, row stride) of `count` parameters at `offset` of every row of X or G."""
+    torch = _torch or _use_torch()
+    if t.dim() != len(lead) + 1 or tuple(t.shape[:-1]) != lead:
+        raise ValueError(f"{name} must be {list(lead) + ['row']}")
+    ld = t.shape[-1]
+    if offset < 0 or offset + count > ld:
+        raise ValueError(f"{name}: {count} floats at {offset} do not fit rows of {ld}")
+    return _whole(t, name, torch.float32, t.shape) + 4 * offset, ld
+
+
+class _On:
+    """The call's device: every tensor is on one, which is made the current one for the call."""
+
+    def __init__(self, *tensors):
+        torch = _torch or _use_torch()
+        device = tensors[0].device
+        for t in tensors[1:]:
+            if t is not None and t.device != device:
+                raise ValueError(f"tensors on {device} and {t.device}")
+        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _workspace(t):
+    return (None, 0) if t is None else _ws(t)
+
+
+def embed(X, offset: int, vocab: int, tokens, mask, Y, scale: float = 1.0, stream=None):
+    """Y[i, j, t] = scale * E_i[tokens[i, j, t]], the table E_i [vocab, dim] at ``offset`` of row i
+    of X [n, ld]; tokens int32 [n, m, T], Y [n, m, T, dim] float32 or bfloat16 rows.  Tokens
+    outside [0, vocab) give zeros; unfinished mini-batches (mask [n, m]) are left alone."""
+    n, m, T = tokens.shape
+    torch = _torch or _use_torch()
+    y, ldy, dtype = _rows(Y, "Y", (n, m, T))
+    dim = Y.shape[-1]
+    e, ld = _params(X, "X", (n,), offset, vocab * dim)
+    tok = _whole(tokens, "tokens", torch.int32, (n, m, T))
+    with _On(X, tokens, Y):
+        _check(load().nbsgd_embed(e, ld, n, m, vocab, dim, scale, tok, T, _u8(mask, (n, m)), y, ldy, dtype,
+                                  _stream(X, stream)))
+
+
+def embed_workspace_bytes(n: int, m: int, T: int, vocab: int, dim: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load().nbsgd_embed_workspace_bytes(n, m, T, vocab, dim, ctypes.byref(b)))
+    return b.value
+
+
+def embed_grad(dY, tokens, mask, G, offset: int, vocab: int, workspace, scale: float = 1.0, stream=None):
+    """The table's gradient, scale * the sum of a token's rows of dY [n, m, T, dim], every row of
+    the table, at ``offset`` of the rows of G [n, m, ld]."""
+    n, m, T = tokens.shape
+    torch = _torch or _use_torch()
+    d, ldy, dtype = _rows(dY, "dY", (n, m, T))
+    dim = dY.shape[-1]
+    g, ld = _params(G, "G", (n, m), offset, vocab * dim)
+    tok = _whole(tokens, "tokens", torch.int32, (n, m, T))
+    ws, ws_bytes = _workspace(workspace)
+    with _On(G, tokens, dY, workspace):
+        _check(load().nbsgd_embed_grad(d, ldy, dtype, n, m, T, tok, vocab, dim, scale, _u8(mask, (n, m)), g,
+                                       ld, ws, ws_bytes, _stream(G, stream)))
+
+
+def scan_workspace_bytes(n: int, m: int, batch: int, T: int, dim: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load().nbsgd_scan_workspace_bytes(n, m, batch, T, dim, ctypes.byref(b)))
+    return b.value
+
+
+def _scan_args(x, g, X, offset, lengths, states):
+    torch = _torch or _use_torch()
+    n, m, b, T, dim = x.shape
+    lead = (n, m, b, T)
+    px, ldx, dtype = _rows(x, "x", lead)
+    pg, ldg, _ = _rows(g, "g", lead, dim, x)
+    if ldg != ldx:
+        raise ValueError("x and g must have one row stride")
+    bias, ld = (None, dim) if X is None else _params(X, "X", (n,), offset, dim)
+    f32 = torch.float32
+    return (lead, dim, px, pg, ldx, dtype, bias, ld,
+            _whole(lengths, "lengths", torch.int32, (n, m, b)),
+            _whole(states, "states", f32, (n, m, b, -(-T // SCAN_INTERVAL), dim)))
+
+
+def scan(x, g, mask, h, X=None, offset: int = 0, h0=None, h_last=None, lengths=None, states=None,
+         workspace=None, stream=None):
+    """The gated recurrence h_t = a h_{t-1} + (1 - a) x_t, a = sigmoid(g + bias), over x, g and h
+    [n, m, batch, T, dim] (float32 or bfloat16 rows); the bias [dim] at ``offset`` of row i of
+    X [n, ld], or none.  h0 and h_last float32 [n, m, batch, dim] (h_last may be h0), lengths int32
+    [n, m, batch], states float32 [n, m, batch, ceil(T / SCAN_INTERVAL), dim] for the backward pass."""
+    torch = _torch or _use_torch()
+    (lead, dim, px, pg, ldx, dtype, bias, ld, lens, st) = _scan_args(x, g, X, offset, lengths, states)
+    ph, ldh, _ = _rows(h, "h", lead, dim, x)
+    n, m, b, T = lead
+    f32 = torch.float32
+    ws, ws_bytes = _workspace(workspace)
+    with _On(x, g, h, X, h0, h_last, lengths, states, workspace):
+        _check(load().nbsgd_scan(px, pg, ldx, dtype, n, m, b, T, dim, bias, ld, lens, _u8(mask, (n, m)),
+                                 _whole(h0, "h0", f32, (n, m, b, dim)), ph, ldh,
+                                 _whole(h_last, "h_last", f32, (n, m, b, dim)), st, ws, ws_bytes,
+                                 _stream(x, stream)))
+
+
+def scan_grad(x, g, states, dh, mask, dx, dg, workspace, X=None, G=None, offset: int = 0, dh_last=None,
+              dh0=None, lengths=None, stream=None):
+    """The backward pass of ``scan``: dx and dg laid out as x and g, dh0 [n, m, batch, dim], and the
+    bias's gradient at ``offset`` of the rows of G [n, m, ld]; X and G have one row stride."""
+    torch = _torch or _use_torch()
+    (lead, dim, px, pg, ldx, dtype, bias, ld, lens, st) = _scan_args(x, g, X, offset, lengths, states)
+    pd, lddh, _ = _rows(dh, "dh", lead, dim, x)
+    pdx, lddx, _ = _rows(dx, "dx", lead, dim, x)
+    pdg, lddg, _ = _rows(dg, "dg", lead, dim, x)
+    n, m, b, T = lead
+    if x.numel() and (lddx != ldx or lddg != ldx):
+        raise ValueError("dx and dg must have the row stride of x and g")
+    gb = None
+    if G is not None:
+        gb, ldg = _params(G, "G", (n, m), offset, dim)
+        if X is not None and ldg != ld:
+            raise ValueError("X and G must have one row stride")
+        ld = ldg
+    f32 = torch.float32
+    ws, ws_bytes = _workspace(workspace)
+    with _On(x, g, states, dh, dx, dg, X, G, dh_last, dh0, lengths, workspace):
+        _check(load().nbsgd_scan_grad(px, pg, ldx, dtype, n, m, b, T, dim, bias, ld, lens, _u8(mask, (n, m)),
+                                      st, pd, lddh, _whole(dh_last, "dh_last", f32, (n, m, b, dim)), pdx,
+                                      pdg, _whole(dh0, "dh0", f32, (n, m, b, dim)), gb, ws, ws_bytes,
+                                      _stream(x, stream)))
+
+
+def act_bytes(T: int, dim: int) -> int:
+    """Bytes of one mini-batch's activations [T, dim] in 8 bits."""
+    b = _i64(0)
+    _check(load().nbsgd_act_bytes(T, dim, ctypes.byref(b)))
+    return b.value
+
+
+def _packed(t, n, m, T, dim):
+    torch = _torch or _use_torch()
+    return _whole(t, "packed", torch.uint8, (n, m, act_bytes(T, dim)))
+
+
+def act_pack(A, mask, packed, stream=None):
+    """A [n, m, T, dim] (float32 or bfloat16 rows) into packed uint8 [n, m, act_bytes(T, dim)]."""
+    n, m, T, dim = A.shape
+    a, lda, dtype = _rows(A, "A", (n, m, T))
+    with _On(A, packed):
+        _check(load().nbsgd_act_pack(a, lda, dtype, n, m, T, dim, _u8(mask, (n, m)),
+                                      _packed(packed, n, m, T, dim), _stream(A, stream)))
+
+
+def act_unpack(packed, mask, A, stream=None):
+    """The values that packed stands for, into A [n, m, T, dim]."""
+    n, m, T, dim = A.shape
+    a, lda, dtype = _rows(A, "A", (n, m, T))
+    with _On(A, packed):
+        _check(load().nbsgd_act_unpack(_packed(packed, n, m, T, dim), n, m, T, dim, _u8(mask, (n, m)), a,
+                                        lda, dtype, _stream(A, stream)))
+
+
+def act_workspace_bytes(n: int, m: int, T: int, dim: int, out: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load().nbsgd_act_workspace_bytes(n, m, T, dim, out, ctypes.byref(b)))
+    return b.value
+
+
+def act_grad(packed, dY, mask, G, offset: int, dim: int, workspace=None, stream=None):
+    """Gradient of W [dim, out] of Y = A W from packed A and dY [n, m, T, out] (bfloat16 rows), at
+    ``offset`` of the rows of G [n, m, ld]."""
+    torch = _torch or _use_torch()
+    n, m, T, out = dY.shape
+    d, ldy, dtype = _rows(dY, "dY", (n, m, T))
+    if dtype != BF16:
+        raise TypeError("dY must be bfloat16")
+    g, ld = _params(G, "G", (n, m), offset, dim * out)
+    ws, ws_bytes = _workspace(workspace)
+    with _On(G, dY, packed, workspace):
+        _check(load().nbsgd_act_grad(_packed(packed, n, m, T, dim), d, ldy, n, m, T, dim, out,
+                                      _u8(mask, (n, m)), g, ld, ws, ws_bytes, _stream(G, stream)))

@@ -7,6 +7,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -43,8 +44,11 @@ def _atomic_link(cmd_prefix, out, verbose):
 
 
 # The host translation units (plain C++, no HIP): the schedule and mixing
-# matrices, MATCHA, the step planner and the MLP shape checks.
-HOST_SOURCES = ("host.cpp", "matcha.cpp", "plan.cpp", "mlp_shape.cpp")
+# matrices, MATCHA, the step planner, the MLP shape checks and those of the token
+# models.
+HOST_SOURCES = ("host.cpp", "matcha.cpp", "plan.cpp", "mlp_shape.cpp", "tokens.cpp")
+# The device translation units.
+HIP_SOURCES = ("step.hip", "mlp.hip", "embed.hip", "scan.hip", "act8.hip")
 # Sanitizers for the host-only test build (g++, no GPU code involved).
 SANITIZE_FLAGS = ["-fsanitize=address,undefined", "-fno-sanitize-recover=all",
                   "-fno-omit-frame-pointer", "-g"]
@@ -59,14 +63,16 @@ def build(verbose: bool = False) -> None:
         _run([cxx, *CXX_FLAGS, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, src), "-o", obj],
              verbose)
         host_objs.append(obj)
-    step_o = os.path.join(OBJ, "step.o")
-    _run([HIPCC, *HIP_FLAGS, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, "step.hip"),
-          "-o", step_o], verbose)
-    mlp_o = os.path.join(OBJ, "mlp.o")
-    _run([HIPCC, *HIP_FLAGS, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, "mlp.hip"),
-          "-o", mlp_o], verbose)
-    _atomic_link([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", *host_objs, step_o, mlp_o],
-                 LIB, verbose)
+    hip_objs = [os.path.join(OBJ, src.replace(".hip", ".o")) for src in HIP_SOURCES]
+
+    def compile_hip(src, obj):
+        _run([HIPCC, *HIP_FLAGS, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, src), "-o", obj],
+             verbose)
+
+    with ThreadPoolExecutor(max_workers=len(HIP_SOURCES)) as pool:
+        list(pool.map(compile_hip, HIP_SOURCES, hip_objs))
+    _atomic_link([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", *host_objs, *hip_objs], LIB,
+                 verbose)
     _atomic_link([HIPCC, *HIP_FLAGS, "-shared", "-I", INCLUDE, os.path.join(ROOT, "synth", "fill.hip")],
                  SYNTH_LIB, verbose)
 

@@ -1,0 +1,97 @@
+// Shared by the token models' calls (embed.hip, scan.hip, act8.hip) and their host checks
+// (tokens.cpp, plain C++): the finished mini-batches of a call, the checks of its buffers
+// and the sizes of its workspaces.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "nbsgd.h"
+
+namespace nbsgd {
+
+constexpr int kMaxGroups = NBSGD_MAX_LEARNERS * NBSGD_MAX_MINIBATCHES;
+
+// The finished mini-batches of a call, in order: i * m + j, two to a word (kernel
+// arguments, read as 32-bit words only).
+struct Groups {
+  int32_t count, m;
+  uint32_t w[kMaxGroups / 2];
+};
+#if defined(__HIP__)
+__device__ __forceinline__ int group_id(const Groups& g, int e) {
+  return (int)((g.w[e >> 1] >> (16 * (e & 1))) & 0xffffu);
+}
+#endif
+
+// Checks n, m and the mask and fills *g.
+nbsgd_status check_groups(int32_t n, int32_t m, const uint8_t* mask, Groups* g);
+
+// Bytes of an element, 0 for an unknown type.
+inline int dtype_size(int32_t dtype) {
+  return dtype == NBSGD_F32 ? 4 : dtype == NBSGD_BF16 ? 2 : 0;
+}
+
+// A buffer of a call: `rows` rows of `width` bytes, `stride` bytes apart.
+struct Rows {
+  const char* name;
+  const void* p;
+  int64_t rows, width, stride;
+};
+// Whether no row of one buffer touches a row of the other; rows that lie side by side
+// with one stride (two halves of a buffer) are apart.
+bool rows_apart(const Rows& a, const Rows& b);
+// Checks that the first `outs` buffers overlap neither each other nor the rest.  Null and
+// empty ones pass.
+nbsgd_status check_apart(const Rows* b, int count, int outs);
+
+// Checks the parameters' row stride and alignment.
+nbsgd_status check_params(const char* name, const void* p, int64_t ld, int64_t params);
+// Checks an activation buffer: stride, width limit, alignment of its element; null only
+// where it has no rows.
+nbsgd_status check_rows(const char* name, const void* p, int64_t rows, int64_t width, int64_t ld,
+                        int elem);
+// Checks a workspace.
+nbsgd_status check_workspace(const void* ws, size_t bytes, size_t need);
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// ---- embeddings: the merged list of a mini-batch's sorted tokens and the table's rows is cut
+// into pieces of kPieceItems (embed.hip)
+constexpr int kPieceItems = 64;
+struct EmbedSpace {
+  int64_t pieces;     // of one mini-batch
+  size_t keys, sorted, flags, parts, total;  // byte offsets, and the whole
+};
+EmbedSpace embed_space(int64_t groups, int64_t T, int64_t vocab, int64_t dim);
+nbsgd_status check_embed(int32_t T, int32_t vocab, int32_t dim);
+
+// ---- recurrence: tiles of NBSGD_SCAN_INTERVAL tokens
+constexpr int kScanTile = NBSGD_SCAN_INTERVAL;
+constexpr int kScanWaves = 8;  // rows of bias-gradient sums that a tile leaves
+struct ScanSpace {
+  int64_t tiles;                      // of one sequence
+  size_t pairs, carry, bias, total;   // byte offsets, and the whole
+};
+ScanSpace scan_space(int64_t seqs, int64_t T, int64_t dim);
+nbsgd_status check_scan(int32_t n, int32_t m, int32_t batch, int32_t T, int32_t dim);
+
+// ---- 8-bit activations
+constexpr int kActBlock = 32;
+struct Act8 {
+  int64_t blocks;        // of 32 tokens
+  int64_t scale, bytes;  // offset of the steps, and bytes of a mini-batch
+};
+inline Act8 act8_layout(int64_t T, int64_t dim) {
+  Act8 a;
+  a.blocks = ceil_div(T, kActBlock);
+  a.scale = a.blocks * dim * kActBlock;
+  a.bytes = (a.scale + ceil_div(a.blocks, 4) * dim * 4 + 15) / 16 * 16;
+  return a;
+}
+nbsgd_status check_act8(int32_t T, int32_t dim);
+// Parts that the tokens of a weight gradient are summed in.
+int act8_splits(int64_t T, int64_t dim, int64_t out);
+size_t act8_space(int64_t groups, int64_t T, int64_t dim, int64_t out);
+
+}  // namespace nbsgd

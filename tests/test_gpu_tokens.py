@@ -1,0 +1,535 @@
+"""The token models' kernels against the fp64 oracle, element by element within the bound that
+the oracle carries beside each result, at the sizes and masks where they can go wrong; then a
+mini-batch in calls of its own and of many, captured and replayed, on another stream, and the
+calls together as a training iteration uses them.
+
+A bf16 result may be off by half a step of bf16 (2^-8 of its size) on top of the bound."""
+
+import numpy as np
+import pytest
+
+import paper_2211_00889_amd as nb
+from oracle import step as ostep
+from oracle import tokens as orc
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8}
+SENTINEL = 7.0
+
+
+def _say(msg):
+    print(f"[case] {msg}", flush=True)
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _close(name, got, want, bound, dtype=F32):
+    """|got - want| <= bound + half a step of the result (and of what rounding the bound adds)."""
+    got = _np(got)
+    room = bound + HALF[dtype] * (np.abs(want) + bound) + 1e-37
+    bad = ~(np.abs(got - want) <= room)
+    assert not bad.any(), (f"{name}: {bad.sum()} of {bad.size} off, worst "
+                           f"{np.nanmax(np.abs(got - want) / room):.3g} of the bound, first at "
+                           f"{np.argwhere(bad)[0].tolist()}: {got[bad][0]} for {want[bad][0]}")
+
+
+def _rows(shape, dtype, gap=0, shift=0, fill=None, rng=None, std=1.0):
+    """A tensor of rows with `gap` untouched elements behind each and `shift` before the first;
+    (view, whole buffer)."""
+    width = shape[-1]
+    rows = int(np.prod(shape[:-1]))
+    whole = torch.full((shift + rows * (width + gap) + 8,), SENTINEL, dtype=dtype, device=DEV)
+    view = whole[shift:shift + rows * (width + gap)].view(*shape[:-1], width + gap)[..., :width]
+    if rng is not None:
+        view.copy_(torch.from_numpy(rng.normal(0, std, shape).astype(np.float32)).to(dtype))
+    elif fill is not None:
+        view.fill_(fill)
+    return view, whole
+
+
+def _gaps_untouched(view, whole):
+    probe = whole.clone()
+    torch.as_strided(probe, view.shape, view.stride(), view.storage_offset()).fill_(SENTINEL)
+    assert (probe == SENTINEL).all(), "written outside the rows"
+
+
+def _mask(rng, n, m):
+    mask = (rng.random((n, m)) < 0.6).astype(np.uint8)
+    mask[rng.integers(n), rng.integers(m)] = 1
+    return mask
+
+
+def _ws(size):
+    return torch.empty(max(size, 16), dtype=torch.uint8, device=DEV)
+
+
+# ------------------------------------------------------------------ embeddings
+EMBED = [
+    # n, m, T, vocab, dim, gap, shift, offset
+    (1, 1, 1, 1, 1, 0, 0, 0), (2, 3, 5, 7, 3, 2, 1, 4), (3, 2, 97, 50, 60, 0, 0, 8), (1, 2, 130, 33, 65, 3, 1, 4),
+    (2, 2, 64, 300, 512, 8, 0, 0), (1, 1, 33, 1000, 513, 1, 3, 4), (2, 1, 300, 20, 1032, 0, 0, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,m,T,vocab,dim,gap,shift,offset", EMBED)
+def test_embed(n, m, T, vocab, dim, gap, shift, offset, dtype):
+    rng = np.random.default_rng(T * dim)
+    _say(f"embed {n}x{m} T={T} vocab={vocab} dim={dim} {dtype}")
+    ld = (offset + vocab * dim + 3) // 4 * 4 + 4
+    X = torch.from_numpy(rng.normal(0, 1, (n, ld)).astype(np.float32)).to(DEV)
+    tok = rng.integers(-1, vocab + 1, (n, m, T)).astype(np.int32)
+    mask = _mask(rng, n, m)
+    Y, whole = _rows((n, m, T, dim), dtype, gap, shift)
+    nb.embed(X, offset, vocab, torch.from_numpy(tok).to(DEV), mask, Y, scale=1.75)
+    for i in range(n):
+        E = _np(X[i, offset:offset + vocab * dim]).reshape(vocab, dim)
+        for j in range(m):
+            if mask[i, j]:
+                want = orc.embed(E, tok[i, j], 1.75)
+                _close("Y", Y[i, j], want, orc.U * np.abs(want), dtype)
+            else:
+                assert (Y[i, j] == SENTINEL).all()
+    _gaps_untouched(Y, whole)
+
+
+def _tokens(rng, kind, shape, vocab):
+    if kind == "uniform":
+        return rng.integers(-1, vocab + 1, shape).astype(np.int32)
+    if kind == "one":      # every token the same: the longest run there is
+        return np.full(shape, vocab // 2, np.int32)
+    if kind == "padding":  # nothing inside the table
+        return np.where(rng.random(shape) < 0.5, -7, vocab + 3).astype(np.int32)
+    return np.minimum(rng.zipf(1.3, shape) - 1, vocab - 1).astype(np.int32)  # "zipf"
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind,n,m,T,vocab,dim,gap,shift", [
+    ("uniform", 1, 1, 1, 1, 1, 0, 0), ("uniform", 2, 2, 0, 9, 5, 0, 0), ("uniform", 2, 3, 97, 50, 60, 0, 0),
+    ("one", 2, 1, 300, 11, 33, 1, 1), ("padding", 1, 2, 70, 13, 24, 0, 0), ("zipf", 2, 2, 1000, 200, 64, 0, 0),
+    ("zipf", 1, 2, 1025, 5000, 12, 4, 2), ("one", 1, 1, 9001, 3, 7, 0, 0), ("zipf", 1, 1, 8192, 700, 20, 0, 0),
+    ("uniform", 1, 1, 8193, 70000, 3, 0, 0), ("zipf", 1, 1, 20011, 333, 17, 3, 1), ("uniform", 1, 2, 40, 1, 520, 0, 0),
+    ("zipf", 1, 1, 500, 64, 1300, 0, 0), ("zipf", 3, 1, 129, 257, 513, 7, 1), ("one", 1, 1, 64, 100, 128, 0, 0),
+    ("uniform", 1, 1, 4097, 66000, 9, 0, 0),
+])
+def test_embed_grad(kind, n, m, T, vocab, dim, gap, shift, dtype):
+    rng = np.random.default_rng(T + dim)
+    _say(f"embed_grad {kind} {n}x{m} T={T} vocab={vocab} dim={dim} {dtype}")
+    tok = _tokens(rng, kind, (n, m, T), vocab)
+    mask = _mask(rng, n, m)
+    dY, _ = _rows((n, m, T, dim), dtype, gap, shift, rng=rng)
+    outside = torch.from_numpy((tok < 0) | (tok >= vocab)).to(DEV)
+    dY[outside] = float("nan")  # rows of padding are not read
+    offset = 4
+    ld = offset + (vocab * dim + 3) // 4 * 4 + 4
+    G = torch.full((n, m, ld), SENTINEL, device=DEV)
+    nb.embed_grad(dY, torch.from_numpy(tok).to(DEV), mask, G, offset, vocab,
+                  _ws(nb.embed_workspace_bytes(n, m, T, vocab, dim)), scale=0.75)
+    for i in range(n):
+        for j in range(m):
+            if mask[i, j]:
+                want, bound = orc.embed_grad(_np(dY[i, j]), tok[i, j], vocab, 0.75)
+                _close("G", G[i, j, offset:offset + vocab * dim].view(vocab, dim), want, bound)
+            else:
+                assert (G[i, j] == SENTINEL).all()
+    assert (G[:, :, :offset] == SENTINEL).all() and (G[:, :, offset + vocab * dim:] == SENTINEL).all()
+
+
+# ------------------------------------------------------------------ recurrence
+SCAN = [
+    # n, m, batch, T, dim, joint, lengths, bias, h0
+    (1, 1, 1, 1, 1, 0, "full", 1, 1), (2, 2, 3, 1, 70, 0, "full", 1, 1), (1, 2, 2, 2, 64, 1, "ragged", 0, 0),
+    (2, 2, 2, 33, 60, 0, "ragged", 1, 1), (1, 1, 2, 16, 9, 1, "ragged", 1, 1), (1, 1, 2, 17, 130, 0, "full", 1, 0),
+    (1, 2, 1, 255, 33, 1, "full", 1, 1), (1, 1, 2, 256, 64, 0, "full", 1, 1), (1, 1, 3, 257, 65, 0, "ragged", 1, 1),
+    (2, 1, 2, 700, 24, 1, "ragged", 1, 1), (1, 1, 1, 1500, 67, 0, "full", 0, 1), (1, 1, 4, 300, 7, 0, "empty", 1, 1),
+    (1, 1, 1, 0, 12, 0, "full", 1, 1), (1, 1, 2, 64, 4, 0, "odd", 1, 1), (1, 1, 1, 5000, 5, 0, "full", 1, 1),
+    (1, 1, 2, 513, 136, 1, "odd", 1, 1), (2, 3, 1, 40, 200, 0, "full", 1, 1),
+]
+
+
+def _scan_inputs(rng, n, m, b, T, C, joint, lengths, bias, h0, dtype):
+    d = {}
+    if joint:
+        xg, _ = _rows((n, m, b, T, 2 * C), dtype, rng=rng)
+        d["x"], d["g"] = xg[..., :C], xg[..., C:]
+    else:
+        d["x"], _ = _rows((n, m, b, T, C), dtype, 3, 1, rng=rng)
+        d["g"], _ = _rows((n, m, b, T, C), dtype, 3, 2, rng=rng)
+    d["X"] = torch.from_numpy(rng.normal(0, 1, (n, (C + 3) // 4 * 4 + 8)).astype(np.float32)).to(DEV)
+    d["X"][:, 4:4 + C] += torch.linspace(-1, 6, C, device=DEV)
+    if not bias:
+        d["X"] = None
+    d["h0"] = torch.from_numpy(rng.normal(0, 1, (n, m, b, C)).astype(np.float32)).to(DEV) if h0 else None
+    lens = {"full": np.full((n, m, b), T), "ragged": rng.integers(0, T + 1, (n, m, b)),
+            "empty": np.zeros((n, m, b)), "odd": np.resize([-3, T + 9], (n, m, b))}[lengths].astype(np.int32)
+    d["lengths"] = None if lengths == "full" else torch.from_numpy(lens).to(DEV)
+    d["len"] = np.clip(lens, 0, T)
+    past = torch.arange(T, device=DEV) >= torch.from_numpy(d["len"]).to(DEV)[..., None]
+    d["past"] = past
+    for k in ("x", "g"):
+        d[k][past] = float("nan")  # not read
+    return d
+
+
+def _scan_call(d, mask, n, m, b, T, C, dtype, states=True):
+    h, whole = _rows((n, m, b, T, C), dtype, 1, 1)
+    last = torch.full((n, m, b, C), SENTINEL, device=DEV)
+    st = torch.full((n, m, b, -(-T // nb.SCAN_INTERVAL), C), SENTINEL, device=DEV) if states else None
+    ws = _ws(nb.scan_workspace_bytes(n, m, b, T, C))
+    nb.scan(d["x"], d["g"], mask, h, X=d["X"], offset=4 if d["X"] is not None else 0, h0=d["h0"], h_last=last,
+            lengths=d["lengths"], states=st, workspace=ws)
+    return h, whole, last, st
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,m,b,T,C,joint,lengths,bias,h0", SCAN)
+def test_scan(n, m, b, T, C, joint, lengths, bias, h0, dtype):
+    rng = np.random.default_rng(T + C)
+    _say(f"scan {n}x{m}x{b} T={T} dim={C} {lengths} {dtype}")
+    d = _scan_inputs(rng, n, m, b, T, C, joint, lengths, bias, h0, dtype)
+    mask = _mask(rng, n, m)
+    h, whole, last, st = _scan_call(d, mask, n, m, b, T, C, dtype)
+    dh, _ = _rows((n, m, b, T, C), dtype, 2, 1, rng=rng)
+    dh[d["past"]] = float("nan")
+    dlast = torch.from_numpy(rng.normal(0, 1, (n, m, b, C)).astype(np.float32)).to(DEV) if h0 else None
+    if joint:
+        dxg, _ = _rows((n, m, b, T, 2 * C), dtype)
+        dx, dg = dxg[..., :C], dxg[..., C:]
+    else:
+        dx, wx = _rows((n, m, b, T, C), dtype, 3, 1)
+        dg, wg = _rows((n, m, b, T, C), dtype, 3, 2)
+    dh0 = torch.full((n, m, b, C), SENTINEL, device=DEV)
+    G = torch.full((n, m, (C + 3) // 4 * 4 + 8), SENTINEL, device=DEV)
+    off = 4 if bias else 0
+    nb.scan_grad(d["x"], d["g"], st, dh, mask, dx, dg, _ws(nb.scan_workspace_bytes(n, m, b, T, C)), X=d["X"], G=G,
+                 offset=off, dh_last=dlast, dh0=dh0, lengths=d["lengths"])
+    for i in range(n):
+        bv = _np(d["X"][i, 4:4 + C]) if bias else np.zeros(C)
+        for j in range(m):
+            if not mask[i, j]:
+                for t in (h[i, j], last[i, j], st[i, j], dx[i, j], dg[i, j], dh0[i, j], G[i, j]):
+                    assert (t == SENTINEL).all()
+                continue
+            db, edb = np.zeros(C), np.zeros(C)
+            for k in range(b):
+                at, L = (i, j, k), int(d["len"][i, j, k])
+                x, g = np.nan_to_num(_np(d["x"][at])), np.nan_to_num(_np(d["g"][at]))
+                s0 = _np(d["h0"][at]) if h0 else np.zeros(C)
+                (ho, before, s), (eh, eb, es) = orc.scan(x, g, bv, s0, L)
+                _close("h", h[at], ho, eh, dtype)
+                _close("h_last", last[at], s, es)
+                _close("states", st[at], before[::nb.SCAN_INTERVAL], eb[::nb.SCAN_INTERVAL])
+                l0 = _np(dlast[at]) if h0 else np.zeros(C)
+                (gx, gg, g0, gb), (ex, eg, e0, egb) = orc.scan_grad(x, g, bv, s0, L, np.nan_to_num(_np(dh[at])), l0)
+                _close("dx", dx[at], gx, ex, dtype)
+                _close("dg", dg[at], gg, eg, dtype)
+                _close("dh0", dh0[at], g0, e0)
+                db, edb = db + gb, edb + egb + b * orc.U * np.abs(gg).sum(0)
+            _close("dbias", G[i, j, off:off + C], db, edb)
+    _gaps_untouched(h, whole)
+    if not joint:
+        _gaps_untouched(dx, wx)
+        _gaps_untouched(dg, wg)
+    assert (G[:, :, off + C:] == SENTINEL).all()
+
+
+def test_scan_extreme_gates():
+    """Gates of 0 and 1, and infinite ones: the state is replaced, kept, and never NaN."""
+    g = torch.tensor([float("inf"), -float("inf"), 200.0, -200.0, 88.0, -104.0, 1e38, -1e38], device=DEV)
+    x = torch.full((1, 1, 1, 8, 3), 2.0, device=DEV)
+    gg = g.view(1, 1, 1, 8, 1).expand(1, 1, 1, 8, 3).contiguous()
+    h = torch.zeros_like(x)
+    st = torch.zeros((1, 1, 1, 1, 3), device=DEV)
+    h0 = torch.full((1, 1, 1, 3), -5.0, device=DEV)
+    ws = _ws(nb.scan_workspace_bytes(1, 1, 1, 8, 3))
+    nb.scan(x, gg, [[1]], h, h0=h0, states=st, workspace=ws)
+    assert _np(h[0, 0, 0, :, 0]).tolist() == [-5.0, 2.0, 2.0, 2.0, 2.0, 2.0, 2.0, 2.0]
+    dh, dx, dg = torch.ones_like(x), torch.empty_like(x), torch.empty_like(x)
+    nb.scan_grad(x, gg, st, dh, [[1]], dx, dg, ws)
+    assert torch.isfinite(dx).all() and torch.isfinite(dg).all()
+    assert dx[0, 0, 0, 1, 0] > 0.9 and dx[0, 0, 0, 0, 0] == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scan_token_by_token(dtype):
+    """Served one token at a time, the state in place, against the whole sequence."""
+    rng = np.random.default_rng(5)
+    b, T, C = 5, 20, 77
+    d = _scan_inputs(rng, 1, 1, b, T, C, 0, "full", 1, 1, dtype)
+    h, _, last, _ = _scan_call(d, [[1]], 1, 1, b, T, C, dtype, states=False)
+    state = d["h0"].clone()
+    ws = _ws(nb.scan_workspace_bytes(1, 1, b, 1, C))
+    for t in range(T):
+        x, g = d["x"][:, :, :, t:t + 1].contiguous(), d["g"][:, :, :, t:t + 1].contiguous()
+        one = torch.empty_like(x)
+        nb.scan(x, g, [[1]], one, X=d["X"], offset=4, h0=state, h_last=state, workspace=ws)
+        for k in range(b):
+            (ho, _, _), (eh, _, _) = orc.scan(_np(d["x"][0, 0, k]), _np(d["g"][0, 0, k]), _np(d["X"][0, 4:4 + C]),
+                                              _np(d["h0"][0, 0, k]), T)
+            _close("h", one[0, 0, k, 0], ho[t], eh[t], dtype)
+    assert torch.allclose(state, last, rtol=1e-5, atol=1e-5)
+
+
+# --------------------------------------------------------- 8-bit activations
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,m,T,dim,gap,shift", [
+    (1, 1, 1, 1, 0, 0), (2, 2, 31, 7, 1, 1), (1, 2, 32, 64, 0, 0), (2, 1, 33, 65, 3, 1), (1, 1, 129, 300, 0, 0),
+    (2, 2, 200, 40, 8, 0), (1, 1, 161, 257, 0, 1), (1, 1, 1000, 8, 0, 0), (1, 1, 70, 1030, 0, 0),
+])
+def test_act_pack(n, m, T, dim, gap, shift, dtype):
+    rng = np.random.default_rng(T * dim)
+    _say(f"act_pack {n}x{m} T={T} dim={dim} {dtype}")
+    A, _ = _rows((n, m, T, dim), dtype, gap, shift, rng=rng)
+    A *= torch.exp(torch.linspace(-20, 20, dim, device=DEV))
+    A[..., 0, :] = 0
+    mask = _mask(rng, n, m)
+    packed = torch.full((n, m, nb.act_bytes(T, dim)), 99, dtype=torch.uint8, device=DEV)
+    nb.act_pack(A, mask, packed)
+    out, whole = _rows((n, m, T, dim), dtype, gap + 1, shift)
+    nb.act_unpack(packed, mask, out)
+    wide = torch.zeros((n, m, T, dim), device=DEV)
+    nb.act_unpack(packed, mask, wide)
+    for i in range(n):
+        for j in range(m):
+            if mask[i, j]:
+                q, step = orc.act8(_np(A[i, j]))
+                assert np.array_equal(_np(out[i, j]), q * step) and np.array_equal(_np(wide[i, j]), q * step)
+                _packed_layout(packed[i, j].cpu().numpy(), q, step, T, dim)
+            else:
+                assert (out[i, j] == SENTINEL).all() and (packed[i, j] == 99).all()
+    _gaps_untouched(out, whole)
+
+
+def _packed_layout(raw, q, step, T, dim):
+    """The documented layout: blocks of 32 tokens, channels, tokens; then steps, four blocks a channel."""
+    blocks = -(-T // 32)
+    want = np.zeros((blocks * 32, dim), np.int8)
+    want[:T] = q
+    want = want.reshape(blocks, 32, dim).transpose(0, 2, 1)
+    assert np.array_equal(raw[:blocks * dim * 32].view(np.int8).reshape(blocks, dim, 32), want)
+    steps = np.zeros((-(-blocks // 4) * 4, dim), np.uint8)
+    steps[:blocks] = (np.log2(step[::32]) + 127).astype(np.uint8)
+    got = raw[blocks * dim * 32:][:steps.size].reshape(-1, dim, 4)
+    assert np.array_equal(got, steps.reshape(-1, 4, dim).transpose(0, 2, 1))
+
+
+def test_act_pack_borders():
+    """Peaks that just reach or just miss 127 steps, the smallest and largest steps, infinities and NaNs."""
+    A = torch.zeros((1, 1, 64, 12), device=DEV)
+    peaks = [127.0, 127.49999, 127.5, 127.50001, 128.0, 2.0 ** -126, 2.0 ** -140, 3.4e38, 2.0 ** 127, 1.0]
+    A[0, 0, 5, :10] = torch.tensor(peaks)
+    A[0, 0, 6, :10] = -A[0, 0, 5, :10] / 3
+    A[0, 0, 40, 10], A[0, 0, 41, 11] = float("inf"), float("nan")
+    packed = torch.zeros((1, 1, nb.act_bytes(64, 12)), dtype=torch.uint8, device=DEV)
+    nb.act_pack(A, [[1]], packed)
+    out = torch.zeros_like(A)
+    nb.act_unpack(packed, [[1]], out)
+    q, step = orc.act8(_np(A[0, 0]))
+    assert np.array_equal(_np(out[0, 0]), q * step, equal_nan=True)
+    assert torch.isnan(out[0, 0, 32:, 10:]).all() and (out[0, 0, :32, 10:] == 0).all()
+
+
+@pytest.mark.parametrize("n,m,T,dim,out,gap,shift", [
+    (1, 1, 1, 1, 1, 0, 0), (2, 2, 0, 5, 6, 0, 0), (2, 2, 77, 96, 50, 0, 0), (1, 2, 32, 16, 64, 0, 0),
+    (2, 1, 33, 70, 33, 3, 1), (1, 1, 129, 300, 130, 0, 0), (1, 1, 500, 128, 256, 8, 0), (1, 1, 64, 257, 260, 0, 0),
+    (1, 1, 100, 520, 300, 4, 4), (3, 2, 200, 64, 128, 0, 0), (1, 1, 9000, 40, 72, 0, 0), (1, 1, 4096, 256, 264, 0, 0),
+    (1, 1, 130, 33, 1030, 1, 0),
+])
+def test_act_grad(n, m, T, dim, out, gap, shift):
+    rng = np.random.default_rng(T + dim + out)
+    _say(f"act_grad {n}x{m} T={T} dim={dim} out={out}")
+    A, _ = _rows((n, m, T, dim), BF16, rng=rng)
+    A *= torch.exp(torch.linspace(-3, 3, dim, device=DEV))
+    dY, _ = _rows((n, m, T, out), BF16, gap, shift, rng=rng)
+    mask = _mask(rng, n, m)
+    packed = torch.full((n, m, nb.act_bytes(T, dim)), 255, dtype=torch.uint8, device=DEV)
+    nb.act_pack(A, mask, packed)
+    offset = 8
+    G = torch.full((n, m, offset + (dim * out + 3) // 4 * 4 + 4), SENTINEL, device=DEV)
+    nb.act_grad(packed, dY, mask, G, offset, dim, _ws(nb.act_workspace_bytes(n, m, T, dim, out)))
+    for i in range(n):
+        for j in range(m):
+            if mask[i, j]:
+                q, step = orc.act8(_np(A[i, j]))
+                want, bound = orc.act_grad(q * step, _np(dY[i, j]))
+                _close("G", G[i, j, offset:offset + dim * out].view(dim, out), want, bound)
+            else:
+                assert (G[i, j] == SENTINEL).all()
+    assert (G[:, :, :offset] == SENTINEL).all() and (G[:, :, offset + dim * out:] == SENTINEL).all()
+
+
+# ------------------------------------------------------------- all of them
+def _one_pass(d, mask, sel=None):
+    """Every call on the mini-batches of `mask`; the outputs by name.  `sel`: only mini-batch
+    (i, j), in buffers of its own."""
+    n, m, T, b, V, D, C = d["sizes"]
+    pick = (lambda t: t) if sel is None else (lambda t: t[sel[0]:sel[0] + 1, sel[1]:sel[1] + 1].contiguous())
+    X = d["X"] if sel is None else d["X"][sel[0]:sel[0] + 1].contiguous()
+    if sel is not None:
+        n, m, mask = 1, 1, np.ones((1, 1), np.uint8)
+    tok, dY, x, g, dh, A = (pick(d[k]) for k in ("tokens", "dY", "x", "g", "dh", "A"))
+    o = {k: torch.full(s, SENTINEL, dtype=t, device=DEV) for k, s, t in (
+        ("Y", (n, m, T, D), BF16), ("G", (n, m, X.shape[1]), F32), ("h", x.shape, x.dtype), ("dx", x.shape, x.dtype),
+        ("dg", x.shape, x.dtype), ("last", (n, m, b, C), F32), ("dh0", (n, m, b, C), F32),
+        ("states", (n, m, b, -(-x.shape[3] // nb.SCAN_INTERVAL), C), F32),
+        ("packed", (n, m, nb.act_bytes(T, D)), torch.uint8))}
+    w = [_ws(nb.embed_workspace_bytes(n, m, T, V, D)), _ws(nb.scan_workspace_bytes(n, m, b, x.shape[3], C)),
+         _ws(nb.act_workspace_bytes(n, m, T, D, D))]
+    o["w"] = w
+
+    def run():
+        nb.embed(X, 0, V, tok, mask, o["Y"], scale=2.0)
+        nb.scan(x, g, mask, o["h"], X=X, offset=V * D, h_last=o["last"], states=o["states"], workspace=w[1])
+        nb.scan_grad(x, g, o["states"], dh, mask, o["dx"], o["dg"], w[1], X=X, G=o["G"], offset=V * D, dh0=o["dh0"])
+        nb.act_pack(A, mask, o["packed"])
+        nb.act_grad(o["packed"], dY, mask, o["G"], V * D + C, D, w[2])
+        nb.embed_grad(dY, tok, mask, o["G"], 0, V, w[0], scale=2.0)
+
+    return run, o
+
+
+def _pass_inputs(seed, n=2, m=3, b=2, L=300, V=77, D=136, C=72):
+    rng = np.random.default_rng(seed)
+    T = b * L
+    d = {"sizes": (n, m, T, b, V, D, C),
+         "X": torch.from_numpy(rng.normal(0, 1, (n, V * D + C + D * D)).astype(np.float32)).to(DEV),
+         "tokens": torch.from_numpy(_tokens(rng, "zipf", (n, m, T), V)).to(DEV)}
+    for k, s in (("dY", (n, m, T, D)), ("A", (n, m, T, D)), ("x", (n, m, b, L, C)), ("g", (n, m, b, L, C)),
+                 ("dh", (n, m, b, L, C))):
+        d[k] = _rows(s, BF16, rng=rng)[0].contiguous()
+    return d
+
+
+OUT = ("Y", "G", "h", "dx", "dg", "last", "dh0", "states", "packed")
+
+
+@pytest.mark.parametrize("L", [12, 300, 2100])
+def test_results_of_a_mini_batch_are_its_own(L):
+    """In a call of all, of some and of its own, bit for bit."""
+    d = _pass_inputs(L, L=L)
+    n, m = d["sizes"][:2]
+    run, whole = _one_pass(d, np.ones((n, m), np.uint8))
+    run()
+    some_mask = np.array([[1, 0, 1], [0, 0, 1]], np.uint8)
+    run, some = _one_pass(d, some_mask)
+    run()
+    for i in range(n):
+        for j in range(m):
+            run, one = _one_pass(d, None, (i, j))
+            run()
+            for k in OUT:
+                assert torch.equal(one[k][0, 0], whole[k][i, j]), (k, i, j)
+                if some_mask[i, j]:
+                    assert torch.equal(some[k][i, j], whole[k][i, j]), (k, i, j)
+
+
+def test_captured_and_replayed():
+    """Captured once, replayed on new inputs with eager calls between, against the eager results."""
+    d = _pass_inputs(1)
+    mask = np.array([[1, 1, 0], [1, 0, 1]], np.uint8)
+    run, o = _one_pass(d, mask)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for seed in range(2, 6):
+        new = _pass_inputs(seed)
+        for k in ("X", "tokens", "dY", "A", "x", "g", "dh"):
+            d[k].copy_(new[k])
+        eager_run, want = _one_pass(new, mask)
+        eager_run()
+        for k in OUT:
+            o[k].fill_(3)
+        graph.replay()
+        torch.cuda.synchronize()
+        done = torch.from_numpy(mask.astype(bool)).to(DEV)
+        for k in OUT:
+            assert torch.equal(o[k][done], want[k][done]), (k, seed)
+
+
+def test_on_another_stream():
+    d = _pass_inputs(7)
+    mask = np.ones((2, 3), np.uint8)
+    run, want = _one_pass(d, mask)
+    run()
+    run, o = _one_pass(d, mask)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        run()
+    s.synchronize()
+    for k in OUT:
+        assert torch.equal(o[k], want[k]), k
+
+
+def test_training_iteration():
+    """Embeddings, a joint projection whose input is kept in 8 bits, the recurrence, a squared loss, and
+    back: every gradient lands in its place of G and the fused step takes it.  Against the same model
+    in float64 with autograd, with the activations' 8-bit values where the kernels use them."""
+    n, m, b, L, V, D, C = 2, 2, 2, 70, 40, 48, 28
+    T, scale = b * L, 3.0
+    oW, oB = V * D, V * D + D * 2 * C
+    P = oB + C
+    rng = np.random.default_rng(11)
+    X = torch.from_numpy(rng.normal(0, 0.2, (n, P)).astype(np.float32)).to(DEV)
+    tok = torch.from_numpy(rng.integers(0, V, (n, m, T)).astype(np.int32)).to(DEV)
+    target = torch.from_numpy(rng.normal(0, 1, (n, m, b, L, C)).astype(np.float32)).to(DEV)
+    mask = np.array([[1, 1], [1, 0]], np.uint8)
+    G = torch.zeros((n, m, P), device=DEV)
+    E = torch.zeros((n, m, T, D), device=DEV)
+    packed = torch.zeros((n, m, nb.act_bytes(T, D)), dtype=torch.uint8, device=DEV)
+    nb.embed(X, 0, V, tok, mask, E, scale=scale)
+    nb.act_pack(E, mask, packed)
+    W = X[:, oW:oB].view(n, 1, D, 2 * C)
+    xg = torch.matmul(E, W).view(n, m, b, L, 2 * C)
+    h = torch.zeros((n, m, b, L, C), device=DEV)
+    states = torch.zeros((n, m, b, 1, C), device=DEV)
+    ws = _ws(nb.scan_workspace_bytes(n, m, b, L, C))
+    nb.scan(xg[..., :C], xg[..., C:], mask, h, X=X, offset=oB, states=states, workspace=ws)
+    dh = (h - target) / T
+    dxg = torch.zeros_like(xg)
+    nb.scan_grad(xg[..., :C], xg[..., C:], states, dh, mask, dxg[..., :C], dxg[..., C:], ws, X=X, G=G, offset=oB)
+    d16 = dxg.view(n, m, T, 2 * C).to(BF16)
+    nb.act_grad(packed, d16, mask, G, oW, D, _ws(nb.act_workspace_bytes(n, m, T, D, 2 * C)))
+    dE = torch.matmul(dxg.view(n, m, T, 2 * C), W.transpose(-1, -2).contiguous())
+    nb.embed_grad(dE, tok, mask, G, 0, V, _ws(nb.embed_workspace_bytes(n, m, T, V, D)), scale=scale)
+    for i in range(n):
+        p = X[i].double().cpu().requires_grad_(True)
+        for j in range(m):
+            if not mask[i, j]:
+                assert (G[i, j] == 0).all()
+                continue
+            p.grad = None
+            Eo = scale * p[:oW].view(V, D)[tok[i, j].long().cpu()]
+            pre = (Eo @ p[oW:oB].view(D, 2 * C)).view(b, L, 2 * C)
+            a, s, hs = torch.sigmoid(pre[..., C:] + p[oB:]), torch.zeros(b, C).double(), []
+            for t in range(L):
+                s = a[:, t] * s + (1 - a[:, t]) * pre[:, t, :C]
+                hs.append(s)
+            pre.retain_grad()
+            (0.5 * (torch.stack(hs, 1) - target[i, j].double().cpu()).pow(2).sum() / T).backward()
+            want, got = p.grad.numpy(), _np(G[i, j])
+            # the projection's gradient from the input's 8-bit values and the bf16 gradient of its output
+            q, st = orc.act8(_np(E[i, j]))
+            dP = pre.grad.view(T, 2 * C).numpy()
+            wW = (q * st).T @ dP
+            # half a step of bf16 in dP; everything else is 32-bit arithmetic
+            room = 2.0 ** -8 * (np.abs(q * st).T @ np.abs(dP)) * 1.01 + 1e-5 * np.abs(wW).max()
+            assert (np.abs(got[oW:oB].reshape(D, 2 * C) - wW) <= room).all()
+            for lo, hi in ((0, oW), (oB, P)):
+                # 32-bit arithmetic through a recurrence of 70 steps and sums of 140 terms: a few
+                # hundred roundings of 2^-24 of the block's largest entry
+                assert np.abs(got[lo:hi] - want[lo:hi]).max() <= 1e-4 * np.abs(want[lo:hi]).max()
+    X0, G0 = _np(X), _np(G)
+    Vm = torch.zeros_like(X)
+    Wm = nb.w_ring(n)
+    nb.step(X, Vm, G, mask, Wm, 0.1, 0.9, nb.MIX_THEN_STEP)
+    Xo, _ = ostep.step(X0, np.zeros((n, P)), G0, mask, Wm, np.float32(0.1), np.float32(0.9), ostep.MIX_THEN_STEP)
+    assert np.abs(_np(X) - Xo).max() <= 1e-5
