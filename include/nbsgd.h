@@ -434,7 +434,7 @@ nbsgd_status nbsgd_mlp_loss(const float *params, const nbsgd_mlp_shape *s, const
  * Activations are `dtype` rows, one row a token, with the rows of a call
  * ld* elements apart in the order mini-batch, (sequence,) token; they need
  * the alignment of their element only, and a row's elements past its width
- * are never touched.  Every sum, softmax-like gate and state is held in fp32;
+ * are never written.  Every sum, softmax-like gate and state is held in fp32;
  * a bf16 result is rounded once, to nearest even.
  * Tokens and lengths are device int32, contiguous.  The device pointers of
  * outputs must not overlap those of inputs or each other (NBSGD_E_ARG), except
@@ -498,7 +498,8 @@ nbsgd_status nbsgd_embed_grad(const void *dY, int64_t ldy, int32_t dtype, int32_
  *          NULL: the state before token 0, 256, 512, ...; what the backward
  *          pass needs besides x and g (h itself is not kept for it)
  * workspace  nbsgd_scan_workspace_bytes, for nbsgd_scan and nbsgd_scan_grad
- * n*m*batch*ceil(dim/64) is at most 2^22 (NBSGD_E_UNSUPPORTED).           */
+ * n*m*batch*ceil(dim/64) and every row stride are at most 2^22
+ * (NBSGD_E_UNSUPPORTED).                                                  */
 #define NBSGD_SCAN_INTERVAL 256
 nbsgd_status nbsgd_scan_workspace_bytes(int32_t n, int32_t m, int32_t batch, int32_t T,
                                         int32_t dim, size_t *bytes);

@@ -101,7 +101,8 @@ def test_sizes_and_mask(name, change, status):
     ("scan", "h", None, _lib.E_ARG), ("scan", "bias", (1 << 41) + 4, _lib.E_ALIGN), ("scan", "ld", 20, _lib.E_SHAPE),
     ("scan", "h0", (1 << 41) + 2, _lib.E_ALIGN), ("scan", "lengths", (1 << 41) + 1, _lib.E_ALIGN),
     ("scan", "workspace", None, _lib.E_ARG), ("scan", "workspace_bytes", 8, _lib.E_ARG),
-    ("scan", "batch", 1 << 21, _lib.E_UNSUPPORTED),
+    ("scan", "batch", 1 << 21, _lib.E_UNSUPPORTED), ("scan", "ldx", (1 << 22) + 1, _lib.E_UNSUPPORTED),
+    ("scan", "ldh", (1 << 22) + 1, _lib.E_UNSUPPORTED), ("scan_grad", "lddh", (1 << 22) + 1, _lib.E_UNSUPPORTED),
     ("scan_grad", "states", None, _lib.E_ARG), ("scan_grad", "dh", None, _lib.E_ARG),
     ("scan_grad", "dx", None, _lib.E_ARG), ("scan_grad", "dg", None, _lib.E_ARG),
     ("scan_grad", "lddh", 2, _lib.E_SHAPE), ("scan_grad", "Gbias", (1 << 41) + 4, _lib.E_ALIGN),
