@@ -21,35 +21,25 @@ using namespace nbsgd;
 
 namespace {
 
-// Gate and complement of z, both accurate where they are small (1 - a would cancel).
+// Gate a = sigmoid(z) and its complement, both accurate where they are small (1 - a would
+// cancel): with e = exp(-|z|) the larger is 1 / (1 + e) and the smaller e / (1 + e).  e is
+// 2^(-|z| log2 e) on the hardware's exponential; EXACT adds what the product's and the
+// constant's rounding lost (|z| 2^-24 of the value otherwise, below bf16's own step).
 struct Gate {
   float a, rest;
 };
-// exp(-|z|) as 2^(z log2 e) on the hardware's exponential; EXACT adds what the product's and
-// the constant's rounding lost (|z| 2^-24 of the value otherwise, below bf16's own step).
 template <bool EXACT>
 __device__ __forceinline__ Gate gate(float z) {
   const float y = -fabsf(z), kL = 1.44269502f, kLlo = 1.92596303e-8f;
   const float t = y * kL;
   float e = __builtin_amdgcn_exp2f(t);
   if constexpr (EXACT) {
-    // an infinite z has e = 0 already
+    // below -200 e is 0 already, and t may be infinite
     const float lost = fmaf(y, kLlo, fmaf(y, kL, -t)) * 0.693147181f;
     e = y > -200.f ? fmaf(e, lost, e) : e;
   }
   const float r = __builtin_amdgcn_rcpf(1.f + e), s = e * r;
   return z >= 0.f ? Gate{r, s} : Gate{s, r};
-}
-// The gate in one register: the smaller of the two, which keeps its accuracy, with z's sign.
-// The other is at least 1/2, so that 1 - s is it to half a step.
-template <bool EXACT>
-__device__ __forceinline__ float fold_gate(float z) {
-  const Gate q = gate<EXACT>(-fabsf(z));
-  return __builtin_copysignf(q.a, z);
-}
-__device__ __forceinline__ Gate unfold_gate(float q) {
-  const float s = fabsf(q), r = 1.f - s;
-  return __builtin_bit_cast(int32_t, q) >= 0 ? Gate{r, s} : Gate{s, r};
 }
 
 // What both passes are told of a call.
@@ -63,11 +53,14 @@ struct Call {
   Groups groups;
 };
 
-// Lanes of a wave over a tile's part: eight lanes hold the CH channels of a token (128 bytes,
-// one cache line), eight such sets take K consecutive tokens each.
+// Lanes of a wave over its 32 tokens of a tile: sixteen lanes hold the CH channels of a token
+// (128 bytes, one cache line; 8 bytes and V channels a lane), four such sets take K
+// consecutive tokens each.  (16 bytes a lane and eight sets of half the tokens took one more
+// step of composition on twice the channels: with everything in flight the arithmetic, not
+// memory, was the bound.)
 template <typename T>
 struct Lanes {
-  static constexpr int V = Elem<T>::V, LV = 8, CH = LV * V, SUBS = 64 / LV, K = 32 / SUBS;
+  static constexpr int V = 8 / sizeof(T), LV = 16, CH = LV * V, SUBS = 64 / LV, K = 32 / SUBS;
 };
 
 struct Where {
@@ -89,8 +82,8 @@ __device__ __forceinline__ Where locate(const Call& c, int block) {
   return w;
 }
 
-// Rows of a tile: a uniform base and 32-bit lane offsets (kMaxStride keeps a tile in them),
-// which leaves a load one address register where 64-bit row pointers took two each.
+// A uniform base and a 32-bit lane offset (kMaxStride keeps it in range): one address register
+// for all the rows of a run, whose bases are uniform too.
 template <typename T>
 __device__ __forceinline__ const T* row_at(const T* base, uint32_t bytes) {
   return reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + bytes);
@@ -99,51 +92,88 @@ template <typename T>
 __device__ __forceinline__ T* row_at(T* base, uint32_t bytes) {
   return reinterpret_cast<T*>(reinterpret_cast<char*>(base) + bytes);
 }
-// Bounds how far the scheduler mixes a run's steps: with all of them under way at once the
-// registers spill.
-__device__ __forceinline__ void step_fence() { __builtin_amdgcn_sched_barrier(0); }
-// Keeps the compiler from holding on to what it derived from v: deriving it again is cheaper
-// than the registers.
-__device__ __forceinline__ float again(float v) {
-  asm("" : "+v"(v));
-  return v;
-}
-__device__ __forceinline__ u32x4 again(u32x4 v) {
-  asm("" : "+v"(v));
-  return v;
-}
 
-// The lane's V biases.
+// The lane's V biases.  -inf becomes the largest finite value (a is 0 all the same), so that
+// the gate of a token past the length, whose g is taken as the largest finite one, stays 1.
 template <int V>
 __device__ __forceinline__ void load_bias(const Call& c, const Where& w, int ch, float (&bias)[V]) {
 #pragma unroll
-  for (int v = 0; v < V; ++v)
+  for (int v = 0; v < V; ++v) {
     bias[v] = c.bias && ch + v < c.dim ? c.bias[(int64_t)(w.id / c.groups.m) * c.ld + ch + v] : 0.f;
+    if (bias[v] == -__builtin_inff()) bias[v] = -3e38f;
+  }
 }
 
-// The lane's rows of one operand, `off` bytes from the tile's first; of them `live` are taken,
-// the others are zeros.  WHOLE (a row is a whole number of 16 bytes): without branches, lanes
-// without a row or a channel read the tile's first 16 bytes instead; the branches for the
-// parts of 16 bytes cost 7,000 instructions and the registers of their addresses.
+// 8 bytes at the alignment of an element.
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ void expand(u32x2 r, float (&v)[4]) {
+  v[0] = bf16_lo(r[0]), v[1] = bf16_hi(r[0]), v[2] = bf16_lo(r[1]), v[3] = bf16_hi(r[1]);
+}
+__device__ __forceinline__ void expand(u32x2 r, float (&v)[2]) {
+  const uint32_t a = r[0], b = r[1];
+  v[0] = __builtin_bit_cast(float, a), v[1] = __builtin_bit_cast(float, b);
+}
+__device__ __forceinline__ u32x2 collapse(const float (&v)[4]) {
+  return (u32x2){pack2(v[0], v[1]), pack2(v[2], v[3])};
+}
+__device__ __forceinline__ u32x2 collapse(const float (&v)[2]) {
+  return (u32x2){__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1])};
+}
+template <typename T>
+struct Word;
+template <>
+struct Word<float> {
+  typedef uint32_t bits;
+  static constexpr uint32_t kPast = 0x7f7fffffu;  // the largest finite values
+};
+template <>
+struct Word<__bf16> {
+  typedef uint16_t bits;
+  static constexpr uint32_t kPast = 0x7f7f7f7fu;
+};
+
+// The K rows from `base`, `ld` elements apart, of a lane `off` bytes into them: the first
+// `live` are read (all of them in a FULL tile), the others are `past` in every word.  WHOLE:
+// rows are a whole number of 8 bytes; otherwise the lane's first n channels are read.
 template <typename T, bool WHOLE>
-__device__ __forceinline__ void load_run(const T* base, const uint32_t (&off)[Lanes<T>::K], int live,
-                                         int n, u32x4 (&r)[Lanes<T>::K]) {
+__device__ __forceinline__ void load_run(const T* base, int64_t ld, uint32_t off, bool full, int live,
+                                         int n, uint32_t past, u32x2 (&r)[Lanes<T>::K]) {
+  constexpr int K = Lanes<T>::K, V = Lanes<T>::V;
+  if (WHOLE && full) {  // uniform
 #pragma unroll
-  for (int k = 0; k < Lanes<T>::K; ++k) {
-    const bool ok = n > 0 && k < live;
-    if constexpr (WHOLE) {
-      const u32x4 v = *reinterpret_cast<const u32x4_any*>(row_at(base, ok ? off[k] : 0u));
+    for (int k = 0; k < K; ++k) r[k] = *reinterpret_cast<const u32x2_any*>(row_at(base + k * ld, off));
+    return;
+  }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) r[k][q] = ok ? v[q] : 0u;
+  for (int k = 0; k < K; ++k) {
+    r[k] = (u32x2){past, past};
+    if (k >= live) continue;
+    const T* p = row_at(base + k * ld, off);
+    if (WHOLE || n >= V) {
+      r[k] = *reinterpret_cast<const u32x2_any*>(p);
     } else {
-      r[k] = ok ? load16<T>(row_at(base, off[k]), n) : (u32x4){0u, 0u, 0u, 0u};
+      typedef typename Word<T>::bits bits;
+      uint32_t w[2] = {0u, 0u};
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (v < n)
+          w[v * sizeof(T) / 4] |= (uint32_t)__builtin_bit_cast(bits, p[v]) << (8 * (v * sizeof(T) % 4));
+      r[k] = (u32x2){w[0], w[1]};
     }
   }
 }
 template <typename T, bool WHOLE>
-__device__ __forceinline__ void store_row(T* p, u32x4 r, int n) {
-  if constexpr (WHOLE) *reinterpret_cast<u32x4_any*>(p) = r;
-  else store16<T>(p, r, n);
+__device__ __forceinline__ void store_row(T* p, u32x2 r, int n) {
+  constexpr int V = Lanes<T>::V;
+  if (WHOLE || n >= V) {
+    *reinterpret_cast<u32x2_any*>(p) = r;
+    return;
+  }
+  typedef typename Word<T>::bits bits;
+  const uint32_t w[2] = {r[0], r[1]};
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    if (v < n) p[v] = __builtin_bit_cast(T, (bits)(w[v * sizeof(T) / 4] >> (8 * (v * sizeof(T) % 4))));
 }
 
 // Inclusive composition of the maps (A, B) over the SUBS lane sets, first to last or last to
@@ -162,7 +192,6 @@ __device__ __forceinline__ void compose(int sub, float (&A)[Lanes<T>::V], float 
       B[v] = take ? fmaf(A[v], pb, B[v]) : B[v];
       A[v] = take ? A[v] * pa : A[v];
     }
-    step_fence();
   }
   const bool first = UP ? sub == 0 : sub == SUBS - 1;
 #pragma unroll
@@ -177,18 +206,18 @@ __device__ __forceinline__ void compose(int sub, float (&A)[Lanes<T>::V], float 
 // V consecutive floats between a lane and LDS.
 template <int V>
 __device__ __forceinline__ void to_lds(float* p, const float (&v)[V]) {
+  typedef float vec __attribute__((ext_vector_type(V)));
+  vec r;
 #pragma unroll
-  for (int q = 0; q < V / 4; ++q)
-    reinterpret_cast<f32x4*>(p)[q] = (f32x4){v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+  for (int k = 0; k < V; ++k) r[k] = v[k];
+  *reinterpret_cast<vec*>(p) = r;
 }
 template <int V>
 __device__ __forceinline__ void from_lds(const float* p, float (&v)[V]) {
+  typedef float vec __attribute__((ext_vector_type(V)));
+  const vec r = *reinterpret_cast<const vec*>(p);
 #pragma unroll
-  for (int q = 0; q < V / 4; ++q) {
-    const f32x4 r = reinterpret_cast<const f32x4*>(p)[q];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[4 * q + k] = r[k];
-  }
+  for (int k = 0; k < V; ++k) v[k] = r[k];
 }
 // Orders the wave's LDS writes before its later reads of other lanes' data.
 __device__ __forceinline__ void wave_fence() {
@@ -231,40 +260,37 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     else if (h0) s = h0[w.seq * c.dim + own];
   }
   const int at = 32 * wave + sub * K;  // the lane's first token of a tile
-  uint32_t ix[K], ih[K];
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    ix[k] = (uint32_t)((at + k) * (int)c.ldx + o) * (uint32_t)sizeof(T);
-    ih[k] = (uint32_t)((at + k) * (int)ldh + o) * (uint32_t)sizeof(T);
-  }
-  u32x4 rx[K], rg[K];
+  const uint32_t col = n > 0 ? o : 0;  // lanes past the last channel read the first ones
+  const uint32_t ix = (uint32_t)(sub * K * (int)c.ldx + (int)col) * (uint32_t)sizeof(T);
+  const uint32_t ih = (uint32_t)(sub * K * (int)ldh + o) * (uint32_t)sizeof(T);
+  u32x2 rx[K], rg[K];
   auto load_tile = [&](int tile) {
     const int t = tile * kScanTile;
-    load_run<T, WHOLE>(x + t * c.ldx, ix, w.len - t - at, n, rx);
-    load_run<T, WHOLE>(g + t * c.ldx, ix, w.len - t - at, n, rg);
+    const int64_t row = (int64_t)(t + 32 * wave) * c.ldx;
+    const bool full = t + kScanTile <= w.len;
+    load_run<T, WHOLE>(x + row, c.ldx, ix, full, w.len - t - at, n, 0u, rx);
+    load_run<T, WHOLE>(g + row, c.ldx, ix, full, w.len - t - at, n, Word<T>::kPast, rg);
   };
   load_tile(tile0);
   for (int tile = tile0; tile < tile1; ++tile) {
     const int t = tile * kScanTile + at, buf = tile & 1;
-    float q[K][V], A[V], B[V];  // gates, folded; 0 (a = 1) past the length
-    u32x4 cx[K];                // this tile's x
+    const bool full = (tile + 1) * kScanTile <= w.len;
+    float a[K][V], b[K][V], A[V], B[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) A[v] = 1.f, B[v] = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float xv[V], gv[V];
-      cx[k] = rx[k];
-      Elem<T>::expand(cx[k], xv);
-      Elem<T>::expand(rg[k], gv);
-      const bool live = t + k < w.len;
+      expand(rx[k], xv);
+      expand(rg[k], gv);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        q[k][v] = live ? fold_gate<sizeof(T) == 4>(gv[v] + bias[v]) : 0.f;
-        const Gate u = unfold_gate(q[k][v]);
-        B[v] = fmaf(u.a, B[v], u.rest * xv[v]);
-        A[v] *= u.a;
+        const Gate u = gate<sizeof(T) == 4>(gv[v] + bias[v]);
+        a[k][v] = u.a;
+        b[k][v] = u.rest * xv[v];
+        B[v] = fmaf(a[k][v], B[v], b[k][v]);
+        A[v] *= a[k][v];
       }
-      step_fence();
     }
     if (tile + 1 < tile1) load_tile(tile + 1);
     float EA[V], EB[V];
@@ -297,51 +323,59 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     wave_fence();
 #pragma unroll
     for (int v = 0; v < V; ++v) hv[v] = fmaf(EA[v], hv[v], EB[v]);
+    T* to = out0 + (int64_t)(tile * kScanTile + 32 * wave) * ldh;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      float out[V], xv[V];
-      Elem<T>::expand(again(cx[k]), xv);
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const Gate u = unfold_gate(again(q[k][v]));
-        hv[v] = fmaf(u.a, hv[v], u.rest * xv[v]);
-        out[v] = t + k < w.len ? hv[v] : 0.f;
-      }
-      if (n > 0 && t + k < c.T)
-        store_row<T, WHOLE>(row_at(out0 + tile * kScanTile * ldh, ih[k]), Elem<T>::collapse(out), n);
-      step_fence();
+      for (int v = 0; v < V; ++v) hv[v] = fmaf(a[k][v], hv[v], b[k][v]);
+      u32x2 r = collapse(hv);
+      if (!full && t + k >= w.len) r = (u32x2){0u, 0u};
+      if (n > 0 && (full || t + k < c.T)) store_row<T, WHOLE>(row_at(to + k * ldh, ih), r, n);
     }
   }
   if (!PAIRS && h_last && tile1 == c.tiles && keeper) h_last[w.seq * c.dim + own] = s;
 }
 
 // State (or gradient, REVERSE) at the start of every tile of a split sequence, from the tiles'
-// compositions.  A channel a thread.
+// compositions, 64 channels a workgroup: eight waves bring 64 tiles' compositions at a time
+// to LDS (the next ones are on their way meanwhile), one wave steps through them.
 template <bool REVERSE>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(512)
     k_scan_carry(Call c, const float* __restrict__ pairs, const float* __restrict__ first,
                  float* __restrict__ carry) {
+  constexpr int W = 8, U = 8;
+  __shared__ f32x2 stage[W * U][64];
   const int cols = (c.dim + 63) / 64, e = blockIdx.x / cols;
-  const int ch = blockIdx.x % cols * 64 + threadIdx.x;
-  if (ch >= c.dim) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int ch = min((int)(blockIdx.x % cols * 64) + lane, c.dim - 1);  // the last one over and over
   const int64_t seq = (int64_t)group_id(c.groups, e / c.batch) * c.batch + e % c.batch;
   const f32x2* p = reinterpret_cast<const f32x2*>(pairs) + seq * c.tiles * c.dim + ch;
   float* out = carry + seq * c.tiles * c.dim + ch;
   float s = first ? first[seq * c.dim + ch] : 0.f;
-  constexpr int U = 8;  // loads under way
-  for (int k0 = 0; k0 < c.tiles; k0 += U) {
-    f32x2 q[U];
+  f32x2 q[U];
+  auto load = [&](int k0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int k = min(k0 + u, c.tiles - 1);
+      const int k = min(k0 + wave * U + u, c.tiles - 1);
       q[u] = p[(int64_t)(REVERSE ? c.tiles - 1 - k : k) * c.dim];
     }
+  };
+  load(0);
+  for (int k0 = 0; k0 < c.tiles; k0 += W * U) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (k0 + u >= c.tiles) break;
-      out[(int64_t)(REVERSE ? c.tiles - 1 - k0 - u : k0 + u) * c.dim] = s;
-      s = fmaf(q[u][0], s, q[u][1]);
+    for (int u = 0; u < U; ++u) stage[wave * U + u][lane] = q[u];
+    __syncthreads();
+    load(k0 + W * U);
+    if (wave == 0) {
+      const int count = min(W * U, c.tiles - k0);
+#pragma unroll 8
+      for (int u = 0; u < count; ++u) {
+        out[(int64_t)(REVERSE ? c.tiles - 1 - k0 - u : k0 + u) * c.dim] = s;
+        const f32x2 r = stage[u][lane];
+        s = fmaf(r[0], s, r[1]);
+      }
     }
+    __syncthreads();
   }
 }
 
@@ -377,56 +411,54 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     else if (dh_last) mu = dh_last[w.seq * c.dim + own];
   }
   const int at = 32 * wave + sub * K;
-  uint32_t ix[K], id[K];
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    ix[k] = (uint32_t)((at + k) * (int)c.ldx + o) * (uint32_t)sizeof(T);
-    id[k] = (uint32_t)((at + k) * (int)lddh + o) * (uint32_t)sizeof(T);
-  }
-  u32x4 rx[K], rg[K], rd[K];
+  const uint32_t col = n > 0 ? o : 0;
+  const uint32_t ix = (uint32_t)(sub * K * (int)c.ldx + (int)col) * (uint32_t)sizeof(T);
+  const uint32_t id = (uint32_t)(sub * K * (int)lddh + (int)col) * (uint32_t)sizeof(T);
+  u32x2 rx[K], rg[K], rd[K];
   float s = 0.f;
   auto load_tile = [&](int tile) {
     const int t = tile * kScanTile;
+    const int64_t row = (int64_t)(t + 32 * wave) * c.ldx;
+    const bool full = t + kScanTile <= w.len;
     if constexpr (!PAIRS) {
-      load_run<T, WHOLE>(x + t * c.ldx, ix, w.len - t - at, n, rx);
+      load_run<T, WHOLE>(x + row, c.ldx, ix, full, w.len - t - at, n, 0u, rx);
       s = own < c.dim ? states[(w.seq * c.tiles + tile) * c.dim + own] : 0.f;
     }
-    load_run<T, WHOLE>(g + t * c.ldx, ix, w.len - t - at, n, rg);
-    load_run<T, WHOLE>(d + t * lddh, id, w.len - t - at, n, rd);
+    load_run<T, WHOLE>(g + row, c.ldx, ix, full, w.len - t - at, n, Word<T>::kPast, rg);
+    load_run<T, WHOLE>(d + (int64_t)(t + 32 * wave) * lddh, lddh, id, full, w.len - t - at, n, 0u, rd);
   };
   load_tile(tile1 - 1);
   for (int tile = tile1 - 1; tile >= tile0; --tile) {
     const int t = tile * kScanTile + at, buf = tile & 1;
-    float q[K][V], A[V], B[V], RA[V], R[V];
-    u32x4 cx[K], cd[K];  // this tile's x and dh, as they came
+    const bool full = (tile + 1) * kScanTile <= w.len;
+    float a[K][V], rest[K][V], A[V], B[V], RA[V], R[V];
+    u32x2 cx[K], cd[K];  // this tile's x and dh, as they came
 #pragma unroll
     for (int v = 0; v < V; ++v) A[v] = 1.f, B[v] = R[v] = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float gv[V], xv[V];
-      Elem<T>::expand(rg[k], gv);
+      expand(rg[k], gv);
       cd[k] = rd[k];
       if constexpr (!PAIRS) {
         cx[k] = rx[k];
-        Elem<T>::expand(cx[k], xv);
+        expand(cx[k], xv);
       }
-      const bool live = t + k < w.len;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        q[k][v] = live ? fold_gate<sizeof(T) == 4>(gv[v] + bias[v]) : 0.f;
-        const Gate u = unfold_gate(q[k][v]);
+        const Gate u = gate<sizeof(T) == 4>(gv[v] + bias[v]);
+        a[k][v] = u.a;
+        rest[k][v] = u.rest;
         if constexpr (!PAIRS) B[v] = fmaf(u.a, B[v], u.rest * xv[v]);
         A[v] *= u.a;
       }
-      step_fence();
     }
 #pragma unroll
     for (int k = K - 1; k >= 0; --k) {
       float dv[V];
-      Elem<T>::expand(again(cd[k]), dv);
+      expand(cd[k], dv);
 #pragma unroll
-      for (int v = 0; v < V; ++v) R[v] = unfold_gate(again(q[k][v])).a * (dv[v] + R[v]);
-      step_fence();
+      for (int v = 0; v < V; ++v) R[v] = a[k][v] * (dv[v] + R[v]);
     }
     const float here = s;
     if (tile > tile0) load_tile(tile - 1);
@@ -483,33 +515,35 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float xv[V];
-      Elem<T>::expand(again(cx[k]), xv);
+      expand(cx[k], xv);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const Gate u = unfold_gate(again(q[k][v]));
         gap[k][v] = hv[v] - xv[v];
-        hv[v] = fmaf(u.a, hv[v], u.rest * xv[v]);
+        hv[v] = fmaf(a[k][v], hv[v], rest[k][v] * xv[v]);
       }
-      step_fence();
     }
+    T *tx = dx0 + (int64_t)(tile * kScanTile + 32 * wave) * c.ldx;
+    T *tg = dg0 + (int64_t)(tile * kScanTile + 32 * wave) * c.ldx;
 #pragma unroll
     for (int k = K - 1; k >= 0; --k) {
       float ox[V], og[V], dv[V];
-      Elem<T>::expand(again(cd[k]), dv);
+      expand(cd[k], dv);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const float lam = dv[v] + m[v];
-        const Gate u = unfold_gate(again(q[k][v]));
-        ox[v] = lam * u.rest;
-        og[v] = ox[v] * u.a * gap[k][v];
-        if (t + k >= w.len) ox[v] = og[v] = 0.f;
-        sum[v] += og[v];
-        m[v] = u.a * lam;
+        ox[v] = lam * rest[k][v];
+        og[v] = ox[v] * a[k][v] * gap[k][v];
+        m[v] = a[k][v] * lam;
       }
-      step_fence();
-      if (n > 0 && t + k < c.T) {
-        store_row<T, WHOLE>(row_at(dx0 + tile * kScanTile * c.ldx, ix[k]), Elem<T>::collapse(ox), n);
-        store_row<T, WHOLE>(row_at(dg0 + tile * kScanTile * c.ldx, ix[k]), Elem<T>::collapse(og), n);
+      if (!full && t + k >= w.len) {  // whatever comes from behind stays behind
+#pragma unroll
+        for (int v = 0; v < V; ++v) ox[v] = og[v] = 0.f;
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) sum[v] += og[v];
+      if (n > 0 && (full || t + k < c.T)) {
+        store_row<T, WHOLE>(row_at(tx + k * c.ldx, ix), collapse(ox), n);
+        store_row<T, WHOLE>(row_at(tg + k * c.ldx, ix), collapse(og), n);
       }
     }
     if (part) {
@@ -691,7 +725,7 @@ nbsgd_status scan_forward(Call& c, const ScanSpace& w, const float* h0, void* h,
     carry = reinterpret_cast<float*>(static_cast<char*>(ws) + w.carry);
     hipLaunchKernelGGL((k_scan<T, true, WHOLE>), grid, block, 0, s, c, h0, nullptr, pairs, out, ldh, nullptr,
                        nullptr);
-    hipLaunchKernelGGL(k_scan_carry<false>, dim3((unsigned)(ceil_div(c.dim, 64) * d.seqs)), dim3(64), 0, s, c, pairs,
+    hipLaunchKernelGGL(k_scan_carry<false>, dim3((unsigned)(ceil_div(c.dim, 64) * d.seqs)), dim3(512), 0, s, c, pairs,
                        h0, carry);
   }
   hipLaunchKernelGGL((k_scan<T, false, WHOLE>), grid, block, 0, s, c, h0, carry, nullptr, out, ldh, h_last,
@@ -724,7 +758,7 @@ nbsgd_status scan_backward(Call& c, const ScanSpace& w, const float* states, con
       carry = reinterpret_cast<float*>(static_cast<char*>(ws) + w.carry);
       hipLaunchKernelGGL((k_scan_grad<T, true, WHOLE>), grid, block, 0, s, c, states, d_in, lddh, dh_last,
                          nullptr, pairs, ox, og, nullptr, nullptr);
-      hipLaunchKernelGGL(k_scan_carry<true>, dim3((unsigned)(ceil_div(c.dim, 64) * d.seqs)), dim3(64), 0, s, c, pairs,
+      hipLaunchKernelGGL(k_scan_carry<true>, dim3((unsigned)(ceil_div(c.dim, 64) * d.seqs)), dim3(512), 0, s, c, pairs,
                          dh_last, carry);
     }
     hipLaunchKernelGGL((k_scan_grad<T, false, WHOLE>), grid, block, 0, s, c, states, d_in, lddh, dh_last, carry,
@@ -774,8 +808,8 @@ extern "C" nbsgd_status nbsgd_scan(const void* x, const void* g, int64_t ldx, in
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   Call c;
   if (nbsgd_status st = fill_call(&c, x, g, ldx, n, m, batch, T, dim, bias, ld, lengths, mask)) return st;
-  const auto run = dtype == NBSGD_F32 ? (dim % 4 ? scan_forward<float, false> : scan_forward<float, true>)
-                                      : (dim % 8 ? scan_forward<__bf16, false> : scan_forward<__bf16, true>);
+  const auto run = dtype == NBSGD_F32 ? (dim % 2 ? scan_forward<float, false> : scan_forward<float, true>)
+                                      : (dim % 4 ? scan_forward<__bf16, false> : scan_forward<__bf16, true>);
   return run(c, w, h0, h, ldh, h_last, states, workspace, s);
 }
 
@@ -824,7 +858,7 @@ extern "C" nbsgd_status nbsgd_scan_grad(const void* x, const void* g, int64_t ld
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   Call c;
   if (nbsgd_status st = fill_call(&c, x, g, ldx, n, m, batch, T, dim, bias, ld, lengths, mask)) return st;
-  const auto run = dtype == NBSGD_F32 ? (dim % 4 ? scan_backward<float, false> : scan_backward<float, true>)
-                                      : (dim % 8 ? scan_backward<__bf16, false> : scan_backward<__bf16, true>);
+  const auto run = dtype == NBSGD_F32 ? (dim % 2 ? scan_backward<float, false> : scan_backward<float, true>)
+                                      : (dim % 4 ? scan_backward<__bf16, false> : scan_backward<__bf16, true>);
   return run(c, w, states, dh, lddh, dh_last, dx, dg, dh0, Gbias, ld, workspace, s);
 }
