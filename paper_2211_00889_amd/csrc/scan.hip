@@ -119,6 +119,12 @@ __device__ __forceinline__ u32x2 collapse(const float (&v)[4]) {
 __device__ __forceinline__ u32x2 collapse(const float (&v)[2]) {
   return (u32x2){__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1])};
 }
+// Keeps the compiler from holding on to what it made of r earlier (32 registers of fp32 for 16
+// of bf16): making it again is cheaper than spilling.
+__device__ __forceinline__ u32x2 again(u32x2 r) {
+  asm("" : "+v"(r));
+  return r;
+}
 template <typename T>
 struct Word;
 template <>
@@ -238,7 +244,9 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
   constexpr int V = L::V, K = L::K, CH = L::CH;
   __shared__ __attribute__((aligned(16))) float tot[2][2][kScanWaves][CH];
   __shared__ __attribute__((aligned(16))) float start[kScanWaves][CH];
-  const Where w = locate<CH>(c, blockIdx.x);
+  // a split sequence's tiles in the reverse of the order that their compositions were made in:
+  // the last ones are in the memory-side cache still
+  const Where w = locate<CH>(c, carry ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = blockDim.x >> 6;
   const int o = lane % L::LV * V, sub = lane / L::LV;
@@ -275,14 +283,33 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
   for (int tile = tile0; tile < tile1; ++tile) {
     const int t = tile * kScanTile + at, buf = tile & 1;
     const bool full = (tile + 1) * kScanTile <= w.len;
+    if (tile * kScanTile >= w.len) {  // uniform: nothing left of the sequence
+      if constexpr (PAIRS) {
+        if (keeper) {
+          const int64_t cell = (w.seq * c.tiles + tile) * c.dim + own;
+          *reinterpret_cast<f32x2*>(pairs + 2 * cell) = (f32x2){1.f, 0.f};
+        }
+      } else {
+        if (states && keeper) states[(w.seq * c.tiles + tile) * c.dim + own] = s;
+        T* to = out0 + (int64_t)(tile * kScanTile + 32 * wave) * ldh;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+          if (n > 0 && t + k < c.T) store_row<T, WHOLE>(row_at(to + k * ldh, ih), (u32x2){0u, 0u}, n);
+      }
+      continue;
+    }
     float a[K][V], b[K][V], A[V], B[V];
+    u32x2 cx[K], cg[K];  // this tile's rows; the next ones are on their way from here on
+#pragma unroll
+    for (int k = 0; k < K; ++k) cx[k] = rx[k], cg[k] = rg[k];
+    if (tile + 1 < tile1) load_tile(tile + 1);
 #pragma unroll
     for (int v = 0; v < V; ++v) A[v] = 1.f, B[v] = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float xv[V], gv[V];
-      expand(rx[k], xv);
-      expand(rg[k], gv);
+      expand(cx[k], xv);
+      expand(cg[k], gv);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const Gate u = gate<sizeof(T) == 4>(gv[v] + bias[v]);
@@ -292,7 +319,6 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
         A[v] *= a[k][v];
       }
     }
-    if (tile + 1 < tile1) load_tile(tile + 1);
     float EA[V], EB[V];
     compose<T, true>(sub, A, B, EA, EB);
     if (sub == L::SUBS - 1) {
@@ -390,7 +416,9 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
   constexpr int V = L::V, K = L::K, CH = L::CH;
   __shared__ __attribute__((aligned(16))) float tot[2][4][kScanWaves][CH];
   __shared__ __attribute__((aligned(16))) float start[kScanWaves][2][CH];
-  const Where w = locate<CH>(c, blockIdx.x);
+  // a split sequence's tiles in the reverse of the order that their compositions were made in:
+  // the last ones are in the memory-side cache still
+  const Where w = locate<CH>(c, carry ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = blockDim.x >> 6;
   const int o = lane % L::LV * V, sub = lane / L::LV;
@@ -431,19 +459,43 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
   for (int tile = tile1 - 1; tile >= tile0; --tile) {
     const int t = tile * kScanTile + at, buf = tile & 1;
     const bool full = (tile + 1) * kScanTile <= w.len;
+    T *tx = dx0 + (int64_t)(tile * kScanTile + 32 * wave) * c.ldx;
+    T *tg = dg0 + (int64_t)(tile * kScanTile + 32 * wave) * c.ldx;
+    float* sums = part + ((w.seq * c.tiles + tile) * waves + wave) * c.dim + w.col + o;
+    if (tile * kScanTile >= w.len) {  // uniform: behind the sequence
+      if constexpr (PAIRS) {
+        if (keeper) {
+          const int64_t cell = (w.seq * c.tiles + tile) * c.dim + own;
+          *reinterpret_cast<f32x2*>(pairs + 2 * cell) = (f32x2){1.f, 0.f};
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+          if (n > 0 && t + k < c.T) {
+            store_row<T, WHOLE>(row_at(tx + k * c.ldx, ix), (u32x2){0u, 0u}, n);
+            store_row<T, WHOLE>(row_at(tg + k * c.ldx, ix), (u32x2){0u, 0u}, n);
+          }
+        if (part && sub == 0)
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            if (v < n) sums[v] = 0.f;
+      }
+      if (tile > tile0) load_tile(tile - 1);
+      continue;
+    }
     float a[K][V], rest[K][V], A[V], B[V], RA[V], R[V];
-    u32x2 cx[K], cd[K];  // this tile's x and dh, as they came
+    u32x2 cx[K], cg[K], cd[K];  // this tile's rows; the next ones are on their way from here on
+    const float here = s;
+#pragma unroll
+    for (int k = 0; k < K; ++k) cx[k] = rx[k], cg[k] = rg[k], cd[k] = rd[k];
+    if (tile > tile0) load_tile(tile - 1);
 #pragma unroll
     for (int v = 0; v < V; ++v) A[v] = 1.f, B[v] = R[v] = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float gv[V], xv[V];
-      expand(rg[k], gv);
-      cd[k] = rd[k];
-      if constexpr (!PAIRS) {
-        cx[k] = rx[k];
-        expand(cx[k], xv);
-      }
+      expand(cg[k], gv);
+      if constexpr (!PAIRS) expand(cx[k], xv);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const Gate u = gate<sizeof(T) == 4>(gv[v] + bias[v]);
@@ -456,12 +508,10 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
 #pragma unroll
     for (int k = K - 1; k >= 0; --k) {
       float dv[V];
-      expand(cd[k], dv);
+      expand(again(cd[k]), dv);
 #pragma unroll
       for (int v = 0; v < V; ++v) R[v] = a[k][v] * (dv[v] + R[v]);
     }
-    const float here = s;
-    if (tile > tile0) load_tile(tile - 1);
 #pragma unroll
     for (int v = 0; v < V; ++v) RA[v] = A[v];
     float EA[V], EB[V], FA[V], FR[V];
@@ -515,19 +565,17 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float xv[V];
-      expand(cx[k], xv);
+      expand(again(cx[k]), xv);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         gap[k][v] = hv[v] - xv[v];
         hv[v] = fmaf(a[k][v], hv[v], rest[k][v] * xv[v]);
       }
     }
-    T *tx = dx0 + (int64_t)(tile * kScanTile + 32 * wave) * c.ldx;
-    T *tg = dg0 + (int64_t)(tile * kScanTile + 32 * wave) * c.ldx;
 #pragma unroll
     for (int k = K - 1; k >= 0; --k) {
       float ox[V], og[V], dv[V];
-      expand(cd[k], dv);
+      expand(again(cd[k]), dv);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const float lam = dv[v] + m[v];
@@ -551,11 +599,10 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       for (int dist = 1; dist < L::SUBS; dist *= 2)
 #pragma unroll
         for (int v = 0; v < V; ++v) sum[v] += __shfl_xor(sum[v], dist * L::LV);
-      if (sub == 0 && n > 0) {
-        float* p = part + ((w.seq * c.tiles + tile) * waves + wave) * c.dim + w.col + o;
+      if (sub == 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v)
-          if (v < n) p[v] = sum[v];
+          if (v < n) sums[v] = sum[v];
       }
     }
   }
