@@ -50,6 +50,7 @@ struct Call {
   int64_t ldx, ld;
   int32_t batch, T, dim, tiles;
   int32_t chunk;           // tiles of a workgroup
+  int32_t items;           // workgroups with work
   Groups groups;
 };
 
@@ -68,9 +69,16 @@ struct Where {
   int64_t seq;
   int len;
 };
+// Workgroup b runs on XCD b % 8: each XCD takes a run of neighbours, so that the column blocks of
+// one row, whose lines they share where rows are not whole lines, go through one L2.  FLIP:
+// in the reverse order.
 template <int CH>
-__device__ __forceinline__ Where locate(const Call& c, int block) {
+__device__ __forceinline__ Where locate(const Call& c, bool flip) {
   Where w;
+  const int per = gridDim.x >> 3, i = blockIdx.x >> 3;
+  const int block = (blockIdx.x & 7) * per + (flip ? per - 1 - i : i);
+  w.seq = -1;
+  if (block >= c.items) return w;
   const int cols = (c.dim + CH - 1) / CH, chunks = (c.tiles + c.chunk - 1) / c.chunk;
   w.col = block % cols * CH;
   const int r = block / cols;
@@ -246,7 +254,8 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
   __shared__ __attribute__((aligned(16))) float start[kScanWaves][CH];
   // a split sequence's tiles in the reverse of the order that their compositions were made in:
   // the last ones are in the memory-side cache still
-  const Where w = locate<CH>(c, carry ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+  const Where w = locate<CH>(c, carry != nullptr);
+  if (w.seq < 0) return;  // uniform
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = blockDim.x >> 6;
   const int o = lane % L::LV * V, sub = lane / L::LV;
@@ -418,7 +427,8 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
   __shared__ __attribute__((aligned(16))) float start[kScanWaves][2][CH];
   // a split sequence's tiles in the reverse of the order that their compositions were made in:
   // the last ones are in the memory-side cache still
-  const Where w = locate<CH>(c, carry ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+  const Where w = locate<CH>(c, carry != nullptr);
+  if (w.seq < 0) return;  // uniform
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = blockDim.x >> 6;
   const int o = lane % L::LV * V, sub = lane / L::LV;
@@ -749,6 +759,7 @@ nbsgd_status fill_call(Call* c, const void* x, const void* g, int64_t ldx, int32
   c->dim = dim;
   c->tiles = (int32_t)ceil_div(Tn, kScanTile);
   c->chunk = c->tiles;
+  c->items = 0;
   return check_groups(n, m, mask, &c->groups);
 }
 
@@ -765,7 +776,8 @@ nbsgd_status scan_forward(Call& c, const ScanSpace& w, const float* h0, void* h,
   }
   const Deal d = deal(c, Lanes<T>::CH);
   c.chunk = d.chunk;
-  const dim3 grid((unsigned)(d.cols * d.seqs * d.chunks)), block(64 * d.waves);
+  c.items = (int32_t)(d.cols * d.seqs * d.chunks);
+  const dim3 grid(8 * (unsigned)ceil_div(c.items, 8)), block(64 * d.waves);
   float* carry = nullptr;
   if (d.chunks > 1) {
     float* pairs = reinterpret_cast<float*>(static_cast<char*>(ws) + w.pairs);
@@ -797,8 +809,9 @@ nbsgd_status scan_backward(Call& c, const ScanSpace& w, const float* states, con
   } else {
     const Deal d = deal(c, Lanes<T>::CH);
     c.chunk = d.chunk;
+    c.items = (int32_t)(d.cols * d.seqs * d.chunks);
     rows *= (int64_t)c.tiles * d.waves;
-    const dim3 grid((unsigned)(d.cols * d.seqs * d.chunks)), block(64 * d.waves);
+    const dim3 grid(8 * (unsigned)ceil_div(c.items, 8)), block(64 * d.waves);
     float* carry = nullptr;
     if (d.chunks > 1) {
       float* pairs = reinterpret_cast<float*>(static_cast<char*>(ws) + w.pairs);
