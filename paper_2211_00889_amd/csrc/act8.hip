@@ -1,6 +1,8 @@
 // Activations kept in 8 bits for the backward pass, and the weight gradient of a layer from
 // them (gfx950).  Packed layout of a mini-batch: block of 32 tokens, channel, 32 int8; then
 // group of four blocks, channel, four step exponents (k + 127; 255 for NaNs).
+#include <algorithm>
+
 #include "device_rows.h"
 
 using namespace nbsgd;
@@ -81,46 +83,231 @@ __global__ void __launch_bounds__(256)
       Elem<T>::store(dst + t * lda, step * (float)(int8_t)(w[t >> 4][(t >> 2) & 3] >> (8 * (t & 3))));
 }
 
-// One wave 16 channels x 64 columns, MFMA 16x16x32 a block of 32 tokens.
-// Operands (lane l, t = 0..7): A[l % 16][8 (l / 16) + t], B[8 (l / 16) + t][l % 16]; result
-// D[4 (l / 16) + t][l % 16], t = 0..3.
-__global__ void __launch_bounds__(64)
-    k_act8_grad_plain(const uint8_t* __restrict__ packed, const __bf16* __restrict__ dY, int64_t ldy,
-                      int Tn, int dim, int out, float* __restrict__ G, int64_t ld, Act8 lay,
-                      Groups groups) {
-  const int lane = threadIdx.x, i = lane & 15, g = lane >> 4;
-  const int64_t id = group_id(groups, blockIdx.z);
-  const int k0 = blockIdx.y * 16, c0 = blockIdx.x * 64;
-  const uint8_t* base = packed + id * lay.bytes;
-  const __bf16* rows = dY + id * Tn * ldy;
-  const int64_t ch = min(k0 + i, dim - 1);
-  f32x4 acc[4] = {};
-  for (int64_t blk = 0; blk < lay.blocks; ++blk) {
-    const u32x2 q = *reinterpret_cast<const u32x2*>(base + (blk * dim + ch) * kActBlock + 8 * g);
-    const float step = step_of(base[lay.scale + ((blk >> 2) * dim + ch) * 4 + (blk & 3)]);
-    bf16x8 a;
+// Weight gradient dW = A^T dY: the tokens are the K of MFMA 16x16x32 (bf16, fp32 sums), a
+// packed block of 32 tokens one step of it.  Operands (lane l, t = 0..7): A[l % 16][8 (l / 16)
+// + t], B[8 (l / 16) + t][l % 16]; result D[4 (l / 16) + t][l % 16], t = 0..3.
+//   A  is packed as the operand wants it, 8 consecutive tokens of a channel: a lane loads its
+//      8 bytes straight from memory (16 channels are 512 contiguous bytes) and makes bf16 of
+//      them, u * 2^k - 128 * 2^k of the byte with its top bit turned, exactly; no LDS
+//   B  (dY) comes a row a token: 64 tokens are staged at a time, a thread turns 8 tokens x 4
+//      columns and writes 16 bytes a column.  Column 4 q + c of the tile is slot c * BN / 4 + q,
+//      so that the writes and the reads of 16 lanes are contiguous and a lane's results of
+//      four fragments are four consecutive columns.
+// A wave takes 16 MT channels x 64 JT columns, WM x WN waves a tile.  Two buffers of B, one
+// barrier a stage; the next stage's loads are under way during this one's products.
+template <int MT, int JT, int WM, int WN>
+struct GradTile {
+  static constexpr int kThreads = 64 * WM * WN, BM = 16 * MT * WM, BN = 64 * JT * WN;
+  static constexpr int kTokens = 64, kOcts = kTokens / 8;
+  static constexpr int kCells = kOcts * BN / 4 / kThreads;  // of 8 tokens x 4 columns, a thread
+};
+
+// What a launch is told: items (mini-batch, part of its tokens, tile), tiles fastest.
+struct GradCall {
+  const uint8_t* packed;
+  const __bf16* dY;
+  float* out;       // G, or the parts
+  int64_t ldy, ld;  // of out: floats from one mini-batch to the next
+  int64_t part;     // floats from one part to the next
+  int32_t T, dim, cols, parts, per;  // per: blocks of a part, a multiple of four
+  int32_t tm, tn, items;
+  Act8 lay;
+  Groups groups;
+};
+
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// Eight bytes of a channel as bf16, on the step 2^(byte - 127).  A byte of 255 makes an infinite
+// step and NaNs of every value: inf - inf.
+__device__ __forceinline__ bf16x8 unpack8(u32x2 q, float step) {
+  const float back = -128.f * step;
+  u32x4 r;
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
-      a[t] = (__bf16)(step * (float)(int8_t)(q[t >> 2] >> (8 * (t & 3))));
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t u = q[h] ^ 0x80808080u;
+    const float f0 = fmaf((float)(u & 0xffu), step, back), f1 = fmaf((float)(u >> 8 & 0xffu), step, back);
+    const float f2 = fmaf((float)(u >> 16 & 0xffu), step, back), f3 = fmaf((float)(u >> 24), step, back);
+    r[2 * h] = pack2(f0, f1);
+    r[2 * h + 1] = pack2(f2, f3);
+  }
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+template <int MT, int JT, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
+  using S = GradTile<MT, JT, WM, WN>;
+  constexpr int BN = S::BN, Q = BN / 4, NC = S::kCells;
+  __shared__ __attribute__((aligned(16))) u32x4 Bs[2][S::kOcts][BN];
+  // an XCD (workgroup b runs on XCD b % 8) takes a run of neighbouring tiles, which read the same
+  // tokens through its L2
+  const int xper = gridDim.x >> 3, item = (blockIdx.x & 7) * xper + (int)(blockIdx.x >> 3);
+  if (item >= c.items) return;  // uniform
+  const int tn = item % c.tn, tm = item / c.tn % c.tm, r = item / (c.tn * c.tm);
+  const int part = r % c.parts;
+  const int64_t id = group_id(c.groups, r / c.parts);
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
+  const int k0 = tm * S::BM + 16 * MT * wm, c0 = tn * BN;
+  const int blk0 = part * c.per, blk1 = min(blk0 + c.per, (int)c.lay.blocks);
+  const int stages = (blk1 - blk0 + 1) / 2;
+
+  const uint8_t* base = c.packed + id * c.lay.bytes;
+  const __bf16* rows = c.dY + id * c.T * c.ldy + c0;
+  uint32_t aoff[MT], soff[MT];  // channels past the last read it: nothing stores what they give
 #pragma unroll
-    for (int f = 0; f < 4; ++f) {
-      const int col = c0 + 16 * f + i;
-      bf16x8 b;
+  for (int a = 0; a < MT; ++a) {
+    const uint32_t ch = (uint32_t)min(k0 + 16 * a + i, c.dim - 1);
+    aoff[a] = ch * kActBlock + 8 * g;
+    soff[a] = ch * 4;
+  }
+  int oct[NC], quad[NC];
+#pragma unroll
+  for (int e = 0; e < NC; ++e) {
+    oct[e] = (tid + e * S::kThreads) / Q;
+    quad[e] = (tid + e * S::kThreads) % Q;
+  }
+  const bool whole = c0 + BN <= c.cols;  // every column of the tile is there
+
+  u32x2 qa[2][MT], rb[NC][8];
+  uint32_t sa[MT];
+  auto load = [&](int st) {
+    const int b = blk0 + 2 * st;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* p = base + (int64_t)min(b + h, blk1 - 1) * c.dim * kActBlock;
+#pragma unroll
+      for (int a = 0; a < MT; ++a) qa[h][a] = *reinterpret_cast<const u32x2*>(p + aoff[a]);
+    }
+    const uint8_t* p = base + c.lay.scale + (int64_t)(b >> 2) * c.dim * 4;
+#pragma unroll
+    for (int a = 0; a < MT; ++a) sa[a] = *reinterpret_cast<const uint32_t*>(p + soff[a]);
+    const int t0 = b * kActBlock;
+    if (whole && t0 + S::kTokens <= c.T) {  // uniform
+#pragma unroll
+      for (int e = 0; e < NC; ++e)
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          rb[e][t] = *reinterpret_cast<const u32x2_any*>(rows + (int64_t)(t0 + 8 * oct[e] + t) * c.ldy +
+                                                         4 * quad[e]);
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < NC; ++e)
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        const int64_t tok = blk * kActBlock + 8 * g + t;
-        b[t] = tok < Tn && col < out ? rows[tok * ldy + col] : (__bf16)0.f;
+        uint32_t w[2] = {0u, 0u};
+        const int tok = t0 + 8 * oct[e] + t, n = c.cols - c0 - 4 * quad[e];
+        const __bf16* q = rows + (int64_t)tok * c.ldy + 4 * quad[e];
+        // tokens of the next part are left to it
+        if (tok < c.T && tok < blk1 * kActBlock)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (k < n) w[k >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, q[k]) << (16 * (k & 1));
+        rb[e][t] = (u32x2){w[0], w[1]};
       }
-      acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc[f], 0, 0, 0);
+  };
+  auto stage = [&](int buf) {
+#pragma unroll
+    for (int e = 0; e < NC; ++e)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        u32x4 v;
+#pragma unroll
+        for (int p = 0; p < 4; ++p)  // tokens 2 p, 2 p + 1 of column k: the same half of two rows
+          v[p] = __builtin_amdgcn_perm(rb[e][2 * p + 1][k >> 1], rb[e][2 * p][k >> 1],
+                                       k & 1 ? 0x07060302u : 0x05040100u);
+        Bs[buf][oct[e]][k * Q + quad[e]] = v;
+      }
+  };
+  f32x4 acc[MT][JT][4];
+#pragma unroll
+  for (int a = 0; a < MT; ++a)
+#pragma unroll
+    for (int j = 0; j < JT; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[a][j][k] = (f32x4){0.f, 0.f, 0.f, 0.f};
+
+  if (stages > 0) {
+    load(0);
+    stage(0);
+  }
+  __syncthreads();
+  for (int st = 0; st < stages; ++st) {
+    const int buf = st & 1;
+    u32x2 q[2][MT];
+    uint32_t sb[MT];
+#pragma unroll
+    for (int a = 0; a < MT; ++a) {
+      q[0][a] = qa[0][a], q[1][a] = qa[1][a];
+      sb[a] = sa[a] >> (16 * (st & 1));
+    }
+    if (st + 1 < stages) load(st + 1);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 A[MT];
+#pragma unroll
+      for (int a = 0; a < MT; ++a)
+        A[a] = unpack8(q[h][a], __builtin_bit_cast(float, (sb[a] >> (8 * h) & 0xffu) << 23));
+#pragma unroll
+      for (int j = 0; j < JT; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const bf16x8 B = __builtin_bit_cast(bf16x8, Bs[buf][4 * h + g][k * Q + 16 * (JT * wn + j) + i]);
+#pragma unroll
+          for (int a = 0; a < MT; ++a)
+            acc[a][j][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[a], B, acc[a][j][k], 0, 0, 0);
+        }
+    }
+    if (st + 1 < stages) {
+      stage(buf ^ 1);
+      __syncthreads();
     }
   }
+  float* out = c.out + id * c.ld + part * c.part;
 #pragma unroll
-  for (int f = 0; f < 4; ++f)
+  for (int a = 0; a < MT; ++a)
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const int k = k0 + 4 * g + t, col = c0 + 16 * f + i;
-      if (k < dim && col < out) G[id * ld + (int64_t)k * out + col] = acc[f][t];
+      const int ch = k0 + 16 * a + 4 * g + t;
+      if (ch >= c.dim) continue;
+#pragma unroll
+      for (int j = 0; j < JT; ++j) {
+        const int col = c0 + 64 * (JT * wn + j) + 4 * i;
+        float* p = out + (int64_t)ch * c.cols + col;
+        if (col + 4 <= c.cols) {
+          *reinterpret_cast<f32x4_any*>(p) =
+              (f32x4){acc[a][j][0][t], acc[a][j][1][t], acc[a][j][2][t], acc[a][j][3][t]};
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (col + k < c.cols) p[k] = acc[a][j][k][t];
+        }
+      }
     }
+}
+
+// The parts' sums in order.
+__global__ void __launch_bounds__(256)
+    k_act8_parts(const float* __restrict__ parts, int count, int64_t size, float* __restrict__ G, int64_t ld,
+                 Groups groups) {
+  const int64_t id = group_id(groups, blockIdx.y);
+  for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < size; k += (int64_t)gridDim.x * 256) {
+    const float* p = parts + id * count * size + k;
+    float sum = p[0];
+    for (int q = 1; q < count; ++q) sum += p[q * size];
+    G[id * ld + k] = sum;
+  }
+}
+
+template <int MT, int JT, int WM, int WN>
+void grad_launch(GradCall c, hipStream_t s) {
+  using S = GradTile<MT, JT, WM, WN>;
+  c.tm = (int32_t)ceil_div(c.dim, S::BM);
+  c.tn = (int32_t)ceil_div(c.cols, S::BN);
+  c.items = c.tm * c.tn * c.parts * c.groups.count;
+  hipLaunchKernelGGL((k_act8_grad<MT, JT, WM, WN>), dim3(8 * (unsigned)ceil_div(c.items, 8)),
+                     dim3(S::kThreads), 0, s, c);
 }
 
 template <typename T>
@@ -142,6 +329,8 @@ nbsgd_status unpack_launch(const void* packed, int32_t Tn, int32_t dim, void* A,
                      dim, static_cast<T*>(A), lda, lay, g);
   return launched("nbsgd_act_unpack");
 }
+
+constexpr int64_t kTileEnough = 256;
 
 // Checks shared by the two directions.
 nbsgd_status check_pack(const void* A, int64_t lda, int32_t dtype, int32_t n, int32_t m, int32_t Tn,
@@ -198,6 +387,9 @@ extern "C" nbsgd_status nbsgd_act_grad(const void* packed, const void* dY, int64
     return fail(out < 1 ? NBSGD_E_SHAPE : NBSGD_E_UNSUPPORTED, "out=%d must lie in [1, %d]", out,
                 NBSGD_MAX_WIDTH);
   const int64_t nm = (int64_t)n * m, rows = nm * T;
+  if (nm * dim * out > (int64_t)1 << 36)
+    return fail(NBSGD_E_UNSUPPORTED, "n*m*dim*out = %lld floats of G exceed 2^36",
+                (long long)(nm * dim * out));
   const Act8 lay = act8_layout(T, dim);
   if (!packed && lay.bytes) return fail(NBSGD_E_ARG, "packed is null");
   if ((uintptr_t)packed & 15) return fail(NBSGD_E_ALIGN, "packed must be 16-byte aligned");
@@ -212,9 +404,31 @@ extern "C" nbsgd_status nbsgd_act_grad(const void* packed, const void* dY, int64
   if (nbsgd_status st = check_apart(b, 4, 2)) return st;
   if (nbsgd_status st = check_stream(stream)) return st;
   if (!g.count) return NBSGD_OK;
-  const dim3 grid((unsigned)ceil_div(out, 64), (unsigned)ceil_div(dim, 16), g.count);
-  hipLaunchKernelGGL(k_act8_grad_plain, grid, dim3(64), 0, reinterpret_cast<hipStream_t>(stream),
-                     static_cast<const uint8_t*>(packed), static_cast<const __bf16*>(dY), ldy, T, dim,
-                     out, G, ld, lay, g);
+  GradCall c;
+  c.packed = static_cast<const uint8_t*>(packed);
+  c.dY = static_cast<const __bf16*>(dY);
+  c.ldy = ldy;
+  c.T = T;
+  c.dim = dim;
+  c.cols = out;
+  c.parts = act8_splits(T, dim, out);
+  c.per = (int32_t)(ceil_div(ceil_div(lay.blocks, c.parts), 4) * 4);
+  c.lay = lay;
+  c.groups = g;
+  const int64_t size = (int64_t)dim * out;
+  float* ws = static_cast<float*>(workspace);
+  c.out = c.parts > 1 ? ws : G;
+  c.ld = c.parts > 1 ? c.parts * size : ld;
+  c.part = size;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  // The largest tile that leaves no CU without one: its products per byte of LDS and of L2 are
+  // the most.
+  const int64_t each = (int64_t)c.parts * g.count;
+  if (each * ceil_div(dim, 256) * ceil_div(out, 256) >= kTileEnough) grad_launch<4, 2, 4, 2>(c, s);
+  else if (each * ceil_div(dim, 128) * ceil_div(out, 128) >= kTileEnough) grad_launch<4, 1, 2, 2>(c, s);
+  else grad_launch<2, 1, 2, 2>(c, s);
+  if (c.parts > 1)
+    hipLaunchKernelGGL(k_act8_parts, dim3((unsigned)std::min<int64_t>(ceil_div(size, 256), 1024), g.count),
+                       dim3(256), 0, s, ws, c.parts, size, G, ld, g);
   return launched("nbsgd_act_grad");
 }

@@ -132,8 +132,8 @@ nbsgd_status check_act8(int32_t T, int32_t dim) {
 }
 
 int act8_splits(int64_t T, int64_t dim, int64_t out) {
-  (void)T, (void)dim, (void)out;
-  return 1;
+  const int64_t tiles = ceil_div(dim, 64) * ceil_div(out, 128);
+  return (int)std::max<int64_t>(1, std::min(kSplitTiles / tiles, T / kSplitTokens));
 }
 
 size_t act8_space(int64_t groups, int64_t T, int64_t dim, int64_t out) {

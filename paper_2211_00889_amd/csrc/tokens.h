@@ -90,7 +90,10 @@ inline Act8 act8_layout(int64_t T, int64_t dim) {
   return a;
 }
 nbsgd_status check_act8(int32_t T, int32_t dim);
-// Parts that the tokens of a weight gradient are summed in.
+// Parts that the tokens of a weight gradient are summed in, by workgroups of their own where
+// its smallest tiles (64 x 128) are few and the tokens many.  By the mini-batch's sizes alone,
+// not by how many mini-batches a call has, so that a result does not depend on the others.
+constexpr int64_t kSplitTiles = 128, kSplitTokens = 1024;
 int act8_splits(int64_t T, int64_t dim, int64_t out);
 size_t act8_space(int64_t groups, int64_t T, int64_t dim, int64_t out);
 

@@ -137,6 +137,11 @@ def test_overlap(name, a, b):
     assert b"overlap" in _lib.load().nbsgd_last_error()
 
 
+def test_a_gradient_larger_than_the_memory():
+    assert _call("act_grad", dim=65536, out=65536, ldy=65536, ld=1 << 32, n=5, m=4, mask=_mask(5, 4)) == \
+        _lib.E_UNSUPPORTED
+
+
 def test_rows_side_by_side_do_not_overlap():
     p = 1 << 42
     assert _call("scan_grad", ldx=48, dx=p, dg=p + 48) == _lib.OK
