@@ -555,7 +555,7 @@ nbsgd_status nbsgd_act_unpack(const void *packed, int32_t n, int32_t m, int32_t 
  * dY  bf16 [n][m][T] rows of `out` elements, ldy >= out apart
  * G   device fp32, W's gradient [dim][out] row-major at G + (i*m + j)*ld
  * workspace  nbsgd_act_workspace_bytes(n, m, T, dim, out)
- * n*m*dim*out is at most 2^36 (NBSGD_E_UNSUPPORTED).                      */
+ * n*m*dim*out is at most 2^36 and ldy at most 2^22 (NBSGD_E_UNSUPPORTED). */
 nbsgd_status nbsgd_act_workspace_bytes(int32_t n, int32_t m, int32_t T, int32_t dim, int32_t out,
                                         size_t *bytes);
 nbsgd_status nbsgd_act_grad(const void *packed, const void *dY, int64_t ldy, int32_t n, int32_t m,

@@ -162,10 +162,12 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
     soff[a] = ch * 4;
   }
   int oct[NC], quad[NC];
+  uint32_t boff[NC];  // bytes from a stage's first row; the rows' bases are uniform
 #pragma unroll
   for (int e = 0; e < NC; ++e) {
     oct[e] = (tid + e * S::kThreads) / Q;
     quad[e] = (tid + e * S::kThreads) % Q;
+    boff[e] = 2u * (uint32_t)(8 * oct[e] * (int)c.ldy + 4 * quad[e]);
   }
   const bool whole = c0 + BN <= c.cols;  // every column of the tile is there
 
@@ -185,11 +187,11 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
     const int t0 = b * kActBlock;
     if (whole && t0 + S::kTokens <= c.T) {  // uniform
 #pragma unroll
-      for (int e = 0; e < NC; ++e)
+      for (int t = 0; t < 8; ++t) {
+        const char* row = reinterpret_cast<const char*>(rows + (int64_t)(t0 + t) * c.ldy);
 #pragma unroll
-        for (int t = 0; t < 8; ++t)
-          rb[e][t] = *reinterpret_cast<const u32x2_any*>(rows + (int64_t)(t0 + 8 * oct[e] + t) * c.ldy +
-                                                         4 * quad[e]);
+        for (int e = 0; e < NC; ++e) rb[e][t] = *reinterpret_cast<const u32x2_any*>(row + boff[e]);
+      }
       return;
     }
 #pragma unroll
@@ -331,6 +333,7 @@ nbsgd_status unpack_launch(const void* packed, int32_t Tn, int32_t dim, void* A,
 }
 
 constexpr int64_t kTileEnough = 256;
+constexpr int64_t kMaxStride = 1 << 22;  // 64 rows of dY lie within 32-bit offsets
 
 // Checks shared by the two directions.
 nbsgd_status check_pack(const void* A, int64_t lda, int32_t dtype, int32_t n, int32_t m, int32_t Tn,
@@ -390,6 +393,9 @@ extern "C" nbsgd_status nbsgd_act_grad(const void* packed, const void* dY, int64
   if (nm * dim * out > (int64_t)1 << 36)
     return fail(NBSGD_E_UNSUPPORTED, "n*m*dim*out = %lld floats of G exceed 2^36",
                 (long long)(nm * dim * out));
+  if (ldy > kMaxStride)
+    return fail(NBSGD_E_UNSUPPORTED, "rows of dY: stride %lld exceeds %lld", (long long)ldy,
+                (long long)kMaxStride);
   const Act8 lay = act8_layout(T, dim);
   if (!packed && lay.bytes) return fail(NBSGD_E_ARG, "packed is null");
   if ((uintptr_t)packed & 15) return fail(NBSGD_E_ALIGN, "packed must be 16-byte aligned");
@@ -424,7 +430,7 @@ extern "C" nbsgd_status nbsgd_act_grad(const void* packed, const void* dY, int64
   // The largest tile that leaves no CU without one: its products per byte of LDS and of L2 are
   // the most.
   const int64_t each = (int64_t)c.parts * g.count;
-  if (each * ceil_div(dim, 256) * ceil_div(out, 256) >= kTileEnough) grad_launch<4, 2, 4, 2>(c, s);
+  if (each * ceil_div(dim, 256) * ceil_div(out, 256) >= kTileEnough) grad_launch<2, 4, 8, 1>(c, s);
   else if (each * ceil_div(dim, 128) * ceil_div(out, 128) >= kTileEnough) grad_launch<4, 1, 2, 2>(c, s);
   else grad_launch<2, 1, 2, 2>(c, s);
   if (c.parts > 1)

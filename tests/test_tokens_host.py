@@ -114,7 +114,7 @@ def test_sizes_and_mask(name, change, status):
     ("act_grad", "out", 0, _lib.E_SHAPE), ("act_grad", "out", 65537, _lib.E_UNSUPPORTED),
     ("act_grad", "ld", 380, _lib.E_SHAPE), ("act_grad", "dY", (1 << 41) + 1, _lib.E_ALIGN),
     ("act_grad", "packed", None, _lib.E_ARG), ("act_grad", "G", None, _lib.E_ARG),
-    ("act_grad", "T", 262145, _lib.E_UNSUPPORTED),
+    ("act_grad", "T", 262145, _lib.E_UNSUPPORTED), ("act_grad", "ldy", (1 << 22) + 1, _lib.E_UNSUPPORTED),
 ])
 def test_refusals(name, arg, value, status):
     change = {arg: value}
