@@ -115,7 +115,6 @@ struct GradCall {
   Groups groups;
 };
 
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // Eight bytes of a channel as bf16, on the step 2^(byte - 127).  A byte of 255 makes an infinite

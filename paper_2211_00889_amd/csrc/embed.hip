@@ -36,30 +36,280 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// One wave a row of the table: the mini-batch's tokens are searched 64 at a time and the
-// rows of dY that match are added in their order.
+// ---- gradient of the lookup
+//
+// The tokens of a mini-batch are sorted (k_sort, stable, so that equal tokens keep their order),
+// and the sorted tokens merged with the table's rows 0 .. vocab - 1, a row after the tokens
+// equal to it.  That list is cut into pieces of kPieceItems, one a team of lanes: a team walks
+// its piece, adds the dY row of a token and writes G's row at a row.  So every team has the
+// same work whatever the tokens are, every row of G is written once, and a row whose tokens
+// cross a piece's border is summed from the pieces' parts, in order, by k_embed_join.  What
+// bounds it is the write of G, vocab x dim floats a mini-batch.
+
+// Sorted entry: token in the high word, position in the low; tokens outside the table as vocab.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+
+// Stable sort of up to 1024 x ITEMS tokens of a mini-batch by one workgroup, 8 bits a pass: a
+// wave ranks its tokens against its lanes' equal digits by ballots and its own histogram, the
+// histograms are added over waves and digits, and the tokens go to their places in LDS.
+template <int ITEMS>
+__global__ void __launch_bounds__(kSortThreads)
+    k_sort(const int32_t* __restrict__ tokens, int Tn, int vocab, int bits, uint2* __restrict__ keys,
+           Groups groups) {
+  constexpr int N = kSortThreads * ITEMS;
+  __shared__ uint32_t tok[N];
+  __shared__ uint16_t pos[N];
+  __shared__ uint32_t hist[kSortWaves][256];
+  __shared__ uint32_t wsum[kSortWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t id = group_id(groups, blockIdx.y);
+  const int first = blockIdx.x * N, count = min(N, Tn - first);
+  const int32_t* src = tokens + id * Tn + first;
+  // wave w holds tokens 64 ITEMS w + 64 k + lane, k = 0 .. ITEMS - 1; the ones past the count sort last
+  uint32_t key[ITEMS], at[ITEMS];
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const int p = 64 * (ITEMS * wave + k) + lane;
+    const int32_t t = p < count ? src[p] : 0;
+    key[k] = p >= count ? (uint32_t)vocab + 1 : t >= 0 && t < vocab ? (uint32_t)t : (uint32_t)vocab;
+    at[k] = p;
+  }
+  for (int shift = 0; shift < bits; shift += 8) {
+    for (int k = tid; k < kSortWaves * 256; k += kSortThreads) (&hist[0][0])[k] = 0;
+    __syncthreads();
+    uint32_t rank[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      const uint32_t digit = key[k] >> shift & 0xffu;
+      uint64_t same = ~0ull;  // lanes with this lane's digit
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        const uint64_t set = __ballot(digit >> b & 1);
+        same &= digit >> b & 1 ? set : ~set;
+      }
+      const uint64_t below = same & ((1ull << lane) - 1);
+      const uint32_t before = hist[wave][digit];
+      rank[k] = before + __popcll(below);
+      wave_fence();
+      if (!below) hist[wave][digit] = before + __popcll(same);
+      wave_fence();
+    }
+    __syncthreads();
+    // exclusive sums over (digit, wave): thread (q, d) of four takes waves 4 q .. 4 q + 3 of digit d
+    {
+      const int d = tid >> 2, q = tid & 3;
+      uint32_t v[4], sum = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k] = sum;
+        sum += hist[4 * q + k][d];
+      }
+      uint32_t run = sum;  // inclusive over the wave's threads
+#pragma unroll
+      for (int dist = 1; dist < 64; dist *= 2) {
+        const uint32_t up = __shfl_up(run, dist);
+        if (lane >= dist) run += up;
+      }
+      if (lane == 63) wsum[wave] = run;
+      __syncthreads();
+      uint32_t base = run - sum;
+      for (int k = 0; k < wave; ++k) base += wsum[k];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) hist[4 * q + k][d] = base + v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      const uint32_t to = hist[wave][key[k] >> shift & 0xffu] + rank[k];
+      tok[to] = key[k];
+      pos[to] = (uint16_t)at[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      const int p = 64 * (ITEMS * wave + k) + lane;
+      key[k] = tok[p];
+      at[k] = pos[p];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const int p = 64 * (ITEMS * wave + k) + lane;
+    if (p < count) keys[id * Tn + first + p] = make_uint2(at[k] + first, key[k]);
+  }
+}
+
+// Entries before (token, position) in `count` sorted ones; whole entries are compared, so ties do
+// not exist.
+__device__ __forceinline__ int entries_before(const uint2* s, int count, uint2 e) {
+  int lo = 0, hi = count;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    const uint2 v = s[mid];
+    if (v.y < e.y || (v.y == e.y && v.x < e.x)) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Places of the sorted runs' entries in the whole: an entry's own rank in its run and its rank in
+// each other one.
+__global__ void __launch_bounds__(256)
+    k_sort_join(const uint2* __restrict__ keys, int Tn, int run, uint2* __restrict__ sorted, Groups groups) {
+  const int64_t id = group_id(groups, blockIdx.y);
+  const int p = blockIdx.x * 256 + threadIdx.x;
+  if (p >= Tn) return;
+  const uint2* s = keys + id * Tn;
+  const uint2 e = s[p];
+  int to = p % run;
+  for (int r = 0; r < Tn; r += run)
+    if (r != p / run * run) to += entries_before(s + r, min(run, Tn - r), e);
+  sorted[id * Tn + to] = e;
+}
+
+// Tokens among the first d entries of the merged list of `count` sorted tokens and the rows: the
+// k for which token k - 1 is in (its token <= the rows before it) and token k is not.
+__device__ __forceinline__ int tokens_before(const uint2* s, int count, int vocab, int d) {
+  int lo = max(0, d - vocab), hi = min(d, count);
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    // token mid comes before row d - 1 - mid where it is not above it
+    if (s[mid].y <= (uint32_t)(d - 1 - mid)) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// The first n (at most 4) elements at p, zeros behind them; and back.
+__device__ __forceinline__ void load4(const float* p, int n, float (&v)[4]) {
+  Elem<float>::expand(load16<float>(p, n), v);
+}
+__device__ __forceinline__ void load4(const __bf16* p, int n, float (&v)[4]) {
+  if (n >= 4) {
+    const u32x2 r = *reinterpret_cast<const u32x2_any*>(p);
+    v[0] = bf16_lo(r[0]), v[1] = bf16_hi(r[0]), v[2] = bf16_lo(r[1]), v[3] = bf16_hi(r[1]);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = k < n ? (float)p[k] : 0.f;
+}
+__device__ __forceinline__ void store4(float* p, int n, const float (&v)[4]) {
+  store16<float>(p, Elem<float>::collapse(v), n);
+}
+
+// What the gradient's kernels are told.
+struct GradCall {
+  const uint2* sorted;
+  int32_t* flags;   // per piece: the row that it ended for an earlier piece, or -1
+  float* parts;     // per piece: that row's share of the piece, and the piece's share of the row it leaves
+  float* G;
+  int64_t ldy, ld, pieces;
+  int32_t T, vocab, dim, L;  // L: lanes of a team
+  float scale;
+  Groups groups;
+};
+
+// A team a piece.
 template <typename T>
-__global__ void __launch_bounds__(64)
-    k_embed_rows(const T* __restrict__ dY, int64_t ldy, const int32_t* __restrict__ tokens, int Tn,
-                 int dim, float scale, float* __restrict__ G, int64_t ld, Groups groups) {
-  const int id = group_id(groups, blockIdx.y);
-  const int v = blockIdx.x, lane = threadIdx.x;
-  const int32_t* tok = tokens + (int64_t)id * Tn;
-  const T* rows = dY + (int64_t)id * Tn * ldy;
-  float* out = G + (int64_t)id * ld + (int64_t)v * dim;
-  for (int c0 = 0; c0 < dim; c0 += 64) {
-    const int c = c0 + lane;
-    float sum = 0.f;
-    for (int t0 = 0; t0 < Tn; t0 += 64) {
-      uint64_t hit = __ballot(t0 + lane < Tn && tok[min(t0 + lane, Tn - 1)] == v);
-      while (hit) {
-        const int t = t0 + __builtin_ctzll(hit);
-        hit &= hit - 1;
-        if (c < dim) sum += Elem<T>::load(rows + (int64_t)t * ldy + c);
+__global__ void __launch_bounds__(256) k_embed_grad(const T* __restrict__ dY, GradCall c) {
+  constexpr int V = 4;
+  const int64_t id = group_id(c.groups, blockIdx.y);
+  const int64_t piece = (int64_t)blockIdx.x * (256 / c.L) + threadIdx.x / c.L;
+  if (piece >= c.pieces) return;
+  const int l = threadIdx.x % c.L;
+  const uint2* s = c.sorted + id * c.T;
+  const int d0 = (int)piece * kPieceItems, d1 = min(d0 + kPieceItems, c.T + c.vocab);
+  const int k0 = tokens_before(s, c.T, c.vocab, d0), k1 = tokens_before(s, c.T, c.vocab, d1);
+  const int r0 = d0 - k0, r1 = d1 - k1;  // rows of the piece; row r1 is left open
+  const bool carried = k0 > 0 && r0 < c.vocab && s[k0 - 1].y == (uint32_t)r0;
+  if (l == 0) c.flags[id * c.pieces + piece] = carried && r0 < r1 ? r0 : -1;
+  const T* rows = dY + id * c.T * c.ldy;
+  float* G = c.G + id * c.ld;
+  float* part = c.parts + 2 * (id * c.pieces + piece) * c.dim;
+  for (int col = V * l; col < c.dim; col += V * c.L) {
+    const int n = min(V, c.dim - col);
+    int k = k0;
+    for (int r = r0; r <= r1 && r < c.vocab; ++r) {  // tokens outside the table come last
+      float sum[V] = {0.f, 0.f, 0.f, 0.f};
+      const int k_row = k;
+      while (k < k1 && s[k].y == (uint32_t)r) {
+        float e[V];
+        load4(rows + (int64_t)s[k].x * c.ldy + col, n, e);
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += e[v];
+        ++k;
+      }
+      if (r == r1) {  // left open: what the piece has of it
+        if (k > k_row) store4(part + c.dim + col, n, sum);
+      } else if (r == r0 && carried) {
+        store4(part + col, n, sum);
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] *= c.scale;
+        store4(G + (int64_t)r * c.dim + col, n, sum);
       }
     }
-    if (c < dim) out[c] = scale * sum;
   }
+}
+
+// The rows that more than one piece has tokens of: the earlier pieces' parts in order, then the
+// last one's.
+__global__ void __launch_bounds__(256) k_embed_join(GradCall c) {
+  const int64_t id = group_id(c.groups, blockIdx.y), piece = blockIdx.x;
+  const int r = c.flags[id * c.pieces + piece];
+  if (r < 0) return;  // uniform
+  const uint2* s = c.sorted + id * c.T;
+  // the piece with the row's first token
+  const int first = (entries_before(s, c.T, make_uint2(0u, (uint32_t)r)) + r) / kPieceItems;
+  const float* parts = c.parts + 2 * id * c.pieces * c.dim;
+  for (int col = threadIdx.x; col < c.dim; col += 256) {
+    float sum = 0.f;
+#pragma unroll 8
+    for (int64_t q = first; q < piece; ++q) sum += parts[(2 * q + 1) * c.dim + col];
+    c.G[id * c.ld + (int64_t)r * c.dim + col] = c.scale * (sum + parts[2 * piece * c.dim + col]);
+  }
+}
+
+template <int ITEMS>
+void sort_launch(const int32_t* tokens, int32_t T, int32_t vocab, int bits, uint2* keys, const Groups& g,
+                 hipStream_t s) {
+  hipLaunchKernelGGL(k_sort<ITEMS>, dim3((unsigned)ceil_div(T, kSortThreads * ITEMS), g.count),
+                     dim3(kSortThreads), 0, s, tokens, T, vocab, bits, keys, g);
+}
+
+template <typename T>
+void embed_grad_launch(const void* dY, const int32_t* tokens, GradCall c, const EmbedSpace& w, void* ws,
+                       hipStream_t s) {
+  uint2* keys = reinterpret_cast<uint2*>(static_cast<char*>(ws) + w.keys);
+  uint2* sorted = reinterpret_cast<uint2*>(static_cast<char*>(ws) + w.sorted);
+  c.flags = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + w.flags);
+  c.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + w.parts);
+  c.pieces = w.pieces;
+  int bits = 1;
+  while ((c.vocab + 1) >> bits) ++bits;  // of vocab + 1, the largest key
+  int run = kSortThreads;
+  if (!c.T) {
+    // no tokens to sort
+  } else if (c.T <= kSortThreads) {
+    sort_launch<1>(tokens, c.T, c.vocab, bits, keys, c.groups, s);
+  } else if (c.T <= 4 * kSortThreads) {
+    sort_launch<4>(tokens, c.T, c.vocab, bits, keys, c.groups, s);
+    run = 4 * kSortThreads;
+  } else {
+    sort_launch<8>(tokens, c.T, c.vocab, bits, keys, c.groups, s);
+    run = 8 * kSortThreads;
+  }
+  c.sorted = keys;
+  if (c.T > run) {
+    hipLaunchKernelGGL(k_sort_join, dim3((unsigned)ceil_div(c.T, 256), c.groups.count), dim3(256), 0, s,
+                       keys, c.T, run, sorted, c.groups);
+    c.sorted = sorted;
+  }
+  c.L = 16;
+  while (c.L < 128 && c.L * 4 < c.dim) c.L *= 2;
+  hipLaunchKernelGGL(k_embed_grad<T>, dim3((unsigned)ceil_div(c.pieces, 256 / c.L), c.groups.count), dim3(256),
+                     0, s, static_cast<const T*>(dY), c);
+  hipLaunchKernelGGL(k_embed_join, dim3((unsigned)c.pieces, c.groups.count), dim3(256), 0, s, c);
 }
 
 }  // namespace
@@ -122,13 +372,17 @@ extern "C" nbsgd_status nbsgd_embed_grad(const void* dY, int64_t ldy, int32_t dt
   if (nbsgd_status st = check_apart(b, 4, 2)) return st;
   if (nbsgd_status st = check_stream(stream)) return st;
   if (!g.count) return NBSGD_OK;
-  const dim3 grid(vocab, g.count);
+  GradCall c;
+  c.G = G;
+  c.ldy = ldy;
+  c.ld = ld;
+  c.T = T;
+  c.vocab = vocab;
+  c.dim = dim;
+  c.scale = scale;
+  c.groups = g;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (dtype == NBSGD_F32)
-    hipLaunchKernelGGL(k_embed_rows<float>, grid, dim3(64), 0, s, static_cast<const float*>(dY), ldy,
-                       tokens, T, dim, scale, G, ld, g);
-  else
-    hipLaunchKernelGGL(k_embed_rows<__bf16>, grid, dim3(64), 0, s, static_cast<const __bf16*>(dY),
-                       ldy, tokens, T, dim, scale, G, ld, g);
+  if (dtype == NBSGD_F32) embed_grad_launch<float>(dY, tokens, c, w, workspace, s);
+  else embed_grad_launch<__bf16>(dY, tokens, c, w, workspace, s);
   return launched("nbsgd_embed_grad");
 }

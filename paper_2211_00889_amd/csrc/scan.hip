@@ -112,8 +112,6 @@ __device__ __forceinline__ void load_bias(const Call& c, const Where& w, int ch,
   }
 }
 
-// 8 bytes at the alignment of an element.
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 __device__ __forceinline__ void expand(u32x2 r, float (&v)[4]) {
   v[0] = bf16_lo(r[0]), v[1] = bf16_hi(r[0]), v[2] = bf16_lo(r[1]), v[3] = bf16_hi(r[1]);
 }
@@ -233,13 +231,6 @@ __device__ __forceinline__ void from_lds(const float* p, float (&v)[V]) {
 #pragma unroll
   for (int k = 0; k < V; ++k) v[k] = r[k];
 }
-// Orders the wave's LDS writes before its later reads of other lanes' data.
-__device__ __forceinline__ void wave_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // Forward.  PAIRS: only each tile's composition, to `pairs` (the first of the three kernels
 // that split a sequence over workgroups); otherwise the states, from `carry` (the state at the
 // start of every tile) where the sequence is split, else from h0.
