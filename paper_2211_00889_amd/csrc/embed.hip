@@ -167,17 +167,48 @@ __global__ void __launch_bounds__(256)
   sorted[id * Tn + to] = e;
 }
 
-// Tokens among the first d entries of the merged list of `count` sorted tokens and the rows: the
-// k for which token k - 1 is in (its token <= the rows before it) and token k is not.
-__device__ __forceinline__ int tokens_before(const uint2* s, int count, int vocab, int d) {
-  int lo = max(0, d - vocab), hi = min(d, count);
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    // token mid comes before row d - 1 - mid where it is not above it
-    if (s[mid].y <= (uint32_t)(d - 1 - mid)) lo = mid + 1;
-    else hi = mid;
+// Tokens among the first d0 (d1) entries of the merged list of `count` sorted tokens and the
+// rows: token k is entry k + (its token), the rows before it.  Sixteen lanes probe at a time, so
+// that a step leaves a seventeenth (8,192 tokens in four dependent loads, not thirteen), and
+// both searches share the steps.
+__device__ __forceinline__ void tokens_before(const uint2* s, int count, int vocab, int d0, int d1, int* k0,
+                                              int* k1) {
+  const int l = threadIdx.x & 15, base = threadIdx.x & 48;
+  int d[2] = {d0, d1}, lo[2], hi[2];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    lo[q] = max(0, d[q] - vocab);
+    hi[q] = min(d[q], count);
   }
-  return lo;
+  while (__any(lo[0] < hi[0] || lo[1] < hi[1])) {
+    int probe[2];
+    uint32_t tok[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      // 16 places of [lo, hi), ascending; all of a short range, its last one over and over
+      const int n = hi[q] - lo[q];
+      probe[q] = n <= 16 ? min(lo[q] + l, hi[q] - 1) : lo[q] + (int)((int64_t)n * (l + 1) / 17);
+      tok[q] = n > 0 ? s[probe[q]].y : 0u;
+    }
+    int c[2];  // probes 0 .. c - 1 are in
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const bool in = hi[q] > lo[q] && (int)tok[q] <= d[q] - 1 - probe[q];
+      c[q] = __builtin_popcount((uint32_t)(__ballot(in) >> base) & 0xffffu);
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int n = hi[q] - lo[q], from = lo[q];
+      if (n <= 16) {
+        lo[q] = hi[q] = from + min(c[q], max(n, 0));
+      } else {
+        if (c[q]) lo[q] = from + (int)((int64_t)n * c[q] / 17) + 1;
+        if (c[q] < 16) hi[q] = from + (int)((int64_t)n * (c[q] + 1) / 17);
+      }
+    }
+  }
+  *k0 = lo[0];
+  *k1 = lo[1];
 }
 
 // The first n (at most 4) elements at p, zeros behind them; and back.
@@ -197,6 +228,8 @@ __device__ __forceinline__ void store4(float* p, int n, const float (&v)[4]) {
   store16<float>(p, Elem<float>::collapse(v), n);
 }
 
+constexpr int kMinTeam = 16;
+
 // What the gradient's kernels are told.
 struct GradCall {
   const uint2* sorted;
@@ -209,64 +242,114 @@ struct GradCall {
   Groups groups;
 };
 
-// A team a piece.
+// A team a piece: its entries to LDS, then the rows of dY in their order, U of them under way.
 template <typename T>
 __global__ void __launch_bounds__(256) k_embed_grad(const T* __restrict__ dY, GradCall c) {
-  constexpr int V = 4;
+  constexpr int V = 4, U = 8;
+  __shared__ uint2 stage[256 / kMinTeam][kPieceItems + U];
   const int64_t id = group_id(c.groups, blockIdx.y);
-  const int64_t piece = (int64_t)blockIdx.x * (256 / c.L) + threadIdx.x / c.L;
-  if (piece >= c.pieces) return;
-  const int l = threadIdx.x % c.L;
+  const int team = threadIdx.x / c.L, l = threadIdx.x % c.L;
+  // teams past the last piece take it once more and store nothing
+  const int64_t want = (int64_t)blockIdx.x * (256 / c.L) + team;
+  const int64_t piece = min(want, c.pieces - 1);
   const uint2* s = c.sorted + id * c.T;
   const int d0 = (int)piece * kPieceItems, d1 = min(d0 + kPieceItems, c.T + c.vocab);
-  const int k0 = tokens_before(s, c.T, c.vocab, d0), k1 = tokens_before(s, c.T, c.vocab, d1);
+  int k0, k1;
+  tokens_before(s, c.T, c.vocab, d0, d1, &k0, &k1);
   const int r0 = d0 - k0, r1 = d1 - k1;  // rows of the piece; row r1 is left open
+  uint2* mine = stage[team];
+  for (int k = l; k < k1 - k0; k += c.L) mine[k] = s[k0 + k];
   const bool carried = k0 > 0 && r0 < c.vocab && s[k0 - 1].y == (uint32_t)r0;
+  __syncthreads();
+  if (want != piece) return;
   if (l == 0) c.flags[id * c.pieces + piece] = carried && r0 < r1 ? r0 : -1;
+  int count = k1 - k0;
+  if (r1 == c.vocab)  // tokens outside the table come last, and are not read
+    while (count > 0 && mine[count - 1].y == (uint32_t)c.vocab) --count;
   const T* rows = dY + id * c.T * c.ldy;
-  float* G = c.G + id * c.ld;
   float* part = c.parts + 2 * (id * c.pieces + piece) * c.dim;
   for (int col = V * l; col < c.dim; col += V * c.L) {
     const int n = min(V, c.dim - col);
-    int k = k0;
-    for (int r = r0; r <= r1 && r < c.vocab; ++r) {  // tokens outside the table come last
-      float sum[V] = {0.f, 0.f, 0.f, 0.f};
-      const int k_row = k;
-      while (k < k1 && s[k].y == (uint32_t)r) {
-        float e[V];
-        load4(rows + (int64_t)s[k].x * c.ldy + col, n, e);
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] += e[v];
-        ++k;
-      }
-      if (r == r1) {  // left open: what the piece has of it
-        if (k > k_row) store4(part + c.dim + col, n, sum);
-      } else if (r == r0 && carried) {
+    float* to = c.G + id * c.ld + (int64_t)r0 * c.dim + col;
+    float sum[V] = {0.f, 0.f, 0.f, 0.f};
+    int r = r0;
+    auto end_row = [&]() {
+      if (r == r0 && carried) {
         store4(part + col, n, sum);
       } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) sum[v] *= c.scale;
-        store4(G + (int64_t)r * c.dim + col, n, sum);
+        store4(to, n, sum);
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) sum[v] = 0.f;
+      to += c.dim;
+      ++r;
+    };
+    for (int k = 0; k < count; k += U) {
+      float e[U][V];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        load4(rows + (int64_t)mine[min(k + u, count - 1)].x * c.ldy + col, n, e[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (k + u >= count) break;
+        while (r < (int)mine[k + u].y) end_row();
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += e[u][v];
       }
     }
+    while (r < r1) end_row();
+    // left open: what the piece has of it
+    if (r1 < c.vocab && count > 0 && mine[count - 1].y == (uint32_t)r1) store4(part + c.dim + col, n, sum);
   }
 }
 
-// The rows that more than one piece has tokens of: the earlier pieces' parts in order, then the
-// last one's.
+// The rows that more than one piece has tokens of: the earlier pieces' parts, a quarter of them
+// each wave in order, the waves' sums in order, then the last piece's.  Four pieces a workgroup:
+// most of them end no such row.
+constexpr int kJoinPieces = 4;
 __global__ void __launch_bounds__(256) k_embed_join(GradCall c) {
-  const int64_t id = group_id(c.groups, blockIdx.y), piece = blockIdx.x;
-  const int r = c.flags[id * c.pieces + piece];
-  if (r < 0) return;  // uniform
+  __shared__ f32x4 sums[4][64];
+  const int64_t id = group_id(c.groups, blockIdx.y);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint2* s = c.sorted + id * c.T;
-  // the piece with the row's first token
-  const int first = (entries_before(s, c.T, make_uint2(0u, (uint32_t)r)) + r) / kPieceItems;
   const float* parts = c.parts + 2 * id * c.pieces * c.dim;
-  for (int col = threadIdx.x; col < c.dim; col += 256) {
-    float sum = 0.f;
+  for (int64_t piece = (int64_t)blockIdx.x * kJoinPieces;
+       piece < min((int64_t)(blockIdx.x + 1) * kJoinPieces, c.pieces); ++piece) {
+    const int r = c.flags[id * c.pieces + piece];
+    if (r < 0) continue;  // uniform
+    // the piece with the row's first token, and this wave's quarter of those before the last
+    const int first = (entries_before(s, c.T, make_uint2(0u, (uint32_t)r)) + r) / kPieceItems;
+    const int64_t each = (piece - first + 3) / 4, q0 = first + wave * each, q1 = min(q0 + each, piece);
+    for (int c0 = 0; c0 < c.dim; c0 += 256) {
+      const int col = c0 + 4 * lane, n = min(4, c.dim - col);
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      if (n > 0) {
 #pragma unroll 8
-    for (int64_t q = first; q < piece; ++q) sum += parts[(2 * q + 1) * c.dim + col];
-    c.G[id * c.ld + (int64_t)r * c.dim + col] = c.scale * (sum + parts[2 * piece * c.dim + col]);
+        for (int64_t q = q0; q < q1; ++q) {
+          float e[4];
+          load4(parts + (2 * q + 1) * c.dim + col, n, e);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) sum[v] += e[v];
+        }
+      }
+      sums[wave][lane] = (f32x4){sum[0], sum[1], sum[2], sum[3]};
+      __syncthreads();
+      if (wave == 0 && n > 0) {
+        float e[4];
+        load4(parts + 2 * piece * c.dim + col, n, e);
+        for (int w = 1; w < 4; ++w) {
+          const f32x4 t = sums[w][lane];
+#pragma unroll
+          for (int v = 0; v < 4; ++v) sum[v] += t[v];
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sum[v] = c.scale * (sum[v] + e[v]);
+        store4(c.G + id * c.ld + (int64_t)r * c.dim + col, n, sum);
+      }
+      __syncthreads();
+    }
   }
 }
 
@@ -305,11 +388,11 @@ void embed_grad_launch(const void* dY, const int32_t* tokens, GradCall c, const 
                        keys, c.T, run, sorted, c.groups);
     c.sorted = sorted;
   }
-  c.L = 16;
+  c.L = kMinTeam;
   while (c.L < 128 && c.L * 4 < c.dim) c.L *= 2;
   hipLaunchKernelGGL(k_embed_grad<T>, dim3((unsigned)ceil_div(c.pieces, 256 / c.L), c.groups.count), dim3(256),
                      0, s, static_cast<const T*>(dY), c);
-  hipLaunchKernelGGL(k_embed_join, dim3((unsigned)c.pieces, c.groups.count), dim3(256), 0, s, c);
+  hipLaunchKernelGGL(k_embed_join, dim3((unsigned)ceil_div(c.pieces, kJoinPieces), c.groups.count), dim3(256), 0, s, c);
 }
 
 }  // namespace
