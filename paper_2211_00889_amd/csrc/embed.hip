@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(256)
 //
 // The tokens of a mini-batch are sorted (k_sort, stable, so that equal tokens keep their order),
 // and the sorted tokens merged with the table's rows 0 .. vocab - 1, a row after the tokens
-// equal to it.  That list is cut into pieces of kPieceItems, one a team of lanes: a team walks
+// equal to it.  That list is cut into equal pieces, one a team of lanes: a team walks
 // its piece, adds the dY row of a token and writes G's row at a row.  So every team has the
 // same work whatever the tokens are, every row of G is written once, and a row whose tokens
 // cross a piece's border is summed from the pieces' parts, in order, by k_embed_join.  What
@@ -237,7 +237,7 @@ struct GradCall {
   float* parts;     // per piece: that row's share of the piece, and the piece's share of the row it leaves
   float* G;
   int64_t ldy, ld, pieces;
-  int32_t T, vocab, dim, L;  // L: lanes of a team
+  int32_t T, vocab, dim, items, L;  // items of a piece, lanes of a team
   float scale;
   Groups groups;
 };
@@ -246,14 +246,14 @@ struct GradCall {
 template <typename T>
 __global__ void __launch_bounds__(256) k_embed_grad(const T* __restrict__ dY, GradCall c) {
   constexpr int V = 4, U = 8;
-  __shared__ uint2 stage[256 / kMinTeam][kPieceItems + U];
+  __shared__ uint2 stage[256 / kMinTeam][kMaxPiece + U];
   const int64_t id = group_id(c.groups, blockIdx.y);
   const int team = threadIdx.x / c.L, l = threadIdx.x % c.L;
   // teams past the last piece take it once more and store nothing
   const int64_t want = (int64_t)blockIdx.x * (256 / c.L) + team;
   const int64_t piece = min(want, c.pieces - 1);
   const uint2* s = c.sorted + id * c.T;
-  const int d0 = (int)piece * kPieceItems, d1 = min(d0 + kPieceItems, c.T + c.vocab);
+  const int d0 = (int)piece * c.items, d1 = min(d0 + c.items, c.T + c.vocab);
   int k0, k1;
   tokens_before(s, c.T, c.vocab, d0, d1, &k0, &k1);
   const int r0 = d0 - k0, r1 = d1 - k1;  // rows of the piece; row r1 is left open
@@ -279,7 +279,8 @@ __global__ void __launch_bounds__(256) k_embed_grad(const T* __restrict__ dY, Gr
       } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) sum[v] *= c.scale;
-        store4(to, n, sum);
+        if (n == 4) __builtin_nontemporal_store(Elem<float>::collapse(sum), reinterpret_cast<u32x4_any*>(to));
+        else store4(to, n, sum);
       }
 #pragma unroll
       for (int v = 0; v < V; ++v) sum[v] = 0.f;
@@ -320,7 +321,7 @@ __global__ void __launch_bounds__(256) k_embed_join(GradCall c) {
     const int r = c.flags[id * c.pieces + piece];
     if (r < 0) continue;  // uniform
     // the piece with the row's first token, and this wave's quarter of those before the last
-    const int first = (entries_before(s, c.T, make_uint2(0u, (uint32_t)r)) + r) / kPieceItems;
+    const int first = (entries_before(s, c.T, make_uint2(0u, (uint32_t)r)) + r) / c.items;
     const int64_t each = (piece - first + 3) / 4, q0 = first + wave * each, q1 = min(q0 + each, piece);
     for (int c0 = 0; c0 < c.dim; c0 += 256) {
       const int col = c0 + 4 * lane, n = min(4, c.dim - col);
@@ -368,6 +369,7 @@ void embed_grad_launch(const void* dY, const int32_t* tokens, GradCall c, const 
   c.flags = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + w.flags);
   c.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + w.parts);
   c.pieces = w.pieces;
+  c.items = w.items;
   int bits = 1;
   while ((c.vocab + 1) >> bits) ++bits;  // of vocab + 1, the largest key
   int run = kSortThreads;

@@ -57,10 +57,12 @@ nbsgd_status check_workspace(const void* ws, size_t bytes, size_t need);
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ---- embeddings: the merged list of a mini-batch's sorted tokens and the table's rows is cut
-// into pieces of kPieceItems (embed.hip)
-constexpr int kPieceItems = 64;
+// into pieces (embed.hip): of 64 entries, where that gives a mini-batch at least 64 of them,
+// of 16 or 32 where it is small and the time is a piece's own
+constexpr int kMaxPiece = 64;
 struct EmbedSpace {
   int64_t pieces;     // of one mini-batch
+  int32_t items;      // of a piece
   size_t keys, sorted, flags, parts, total;  // byte offsets, and the whole
 };
 EmbedSpace embed_space(int64_t groups, int64_t T, int64_t vocab, int64_t dim);
