@@ -139,31 +139,39 @@ __global__ void __launch_bounds__(kSortThreads)
   }
 }
 
-// Entries before (token, position) in `count` sorted ones; whole entries are compared, so ties do
-// not exist.
-__device__ __forceinline__ int entries_before(const uint2* s, int count, uint2 e) {
-  int lo = 0, hi = count;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    const uint2 v = s[mid];
-    if (v.y < e.y || (v.y == e.y && v.x < e.x)) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo;
-}
-
 // Places of the sorted runs' entries in the whole: an entry's own rank in its run and its rank in
-// each other one.
+// each other one, four runs searched at a time (the steps of one search wait for each other).
+// Whole entries are compared, so there are no ties.
 __global__ void __launch_bounds__(256)
     k_sort_join(const uint2* __restrict__ keys, int Tn, int run, uint2* __restrict__ sorted, Groups groups) {
+  constexpr int U = 4;
   const int64_t id = group_id(groups, blockIdx.y);
   const int p = blockIdx.x * 256 + threadIdx.x;
   if (p >= Tn) return;
   const uint2* s = keys + id * Tn;
   const uint2 e = s[p];
+  const int own = p / run, runs = (Tn + run - 1) / run;
   int to = p % run;
-  for (int r = 0; r < Tn; r += run)
-    if (r != p / run * run) to += entries_before(s + r, min(run, Tn - r), e);
+  for (int r0 = 0; r0 < runs; r0 += U) {
+    int lo[U], hi[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      lo[u] = 0;
+      hi[u] = r0 + u < runs && r0 + u != own ? min(run, Tn - (r0 + u) * run) : 0;
+    }
+    for (int n = run; n > 0; n >>= 1) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (lo[u] >= hi[u]) continue;
+        const int mid = (lo[u] + hi[u]) >> 1;
+        const uint2 v = s[(r0 + u) * run + mid];
+        if (v.y < e.y || (v.y == e.y && v.x < e.x)) lo[u] = mid + 1;
+        else hi[u] = mid;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) to += lo[u];
+  }
   sorted[id * Tn + to] = e;
 }
 
@@ -306,51 +314,42 @@ __global__ void __launch_bounds__(256) k_embed_grad(const T* __restrict__ dY, Gr
   }
 }
 
-// The rows that more than one piece has tokens of: the earlier pieces' parts, a quarter of them
-// each wave in order, the waves' sums in order, then the last piece's.  Four pieces a workgroup:
-// most of them end no such row.
-constexpr int kJoinPieces = 4;
+// The rows that more than one piece has tokens of: the earlier pieces' parts in order, then the
+// last piece's.  A wave a piece; most of them end no such row.
 __global__ void __launch_bounds__(256) k_embed_join(GradCall c) {
-  __shared__ f32x4 sums[4][64];
   const int64_t id = group_id(c.groups, blockIdx.y);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int64_t piece = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (piece >= c.pieces) return;
+  const int r = c.flags[id * c.pieces + piece];
+  if (r < 0) return;  // uniform in the wave
   const uint2* s = c.sorted + id * c.T;
-  const float* parts = c.parts + 2 * id * c.pieces * c.dim;
-  for (int64_t piece = (int64_t)blockIdx.x * kJoinPieces;
-       piece < min((int64_t)(blockIdx.x + 1) * kJoinPieces, c.pieces); ++piece) {
-    const int r = c.flags[id * c.pieces + piece];
-    if (r < 0) continue;  // uniform
-    // the piece with the row's first token, and this wave's quarter of those before the last
-    const int first = (entries_before(s, c.T, make_uint2(0u, (uint32_t)r)) + r) / c.items;
-    const int64_t each = (piece - first + 3) / 4, q0 = first + wave * each, q1 = min(q0 + each, piece);
-    for (int c0 = 0; c0 < c.dim; c0 += 256) {
-      const int col = c0 + 4 * lane, n = min(4, c.dim - col);
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-      if (n > 0) {
-#pragma unroll 8
-        for (int64_t q = q0; q < q1; ++q) {
-          float e[4];
-          load4(parts + (2 * q + 1) * c.dim + col, n, e);
-#pragma unroll
-          for (int v = 0; v < 4; ++v) sum[v] += e[v];
-        }
-      }
-      sums[wave][lane] = (f32x4){sum[0], sum[1], sum[2], sum[3]};
-      __syncthreads();
-      if (wave == 0 && n > 0) {
-        float e[4];
-        load4(parts + 2 * piece * c.dim + col, n, e);
-        for (int w = 1; w < 4; ++w) {
-          const f32x4 t = sums[w][lane];
-#pragma unroll
-          for (int v = 0; v < 4; ++v) sum[v] += t[v];
-        }
-#pragma unroll
-        for (int v = 0; v < 4; ++v) sum[v] = c.scale * (sum[v] + e[v]);
-        store4(c.G + id * c.ld + (int64_t)r * c.dim + col, n, sum);
-      }
-      __syncthreads();
+  int lo = 0, hi = c.T;  // the first token of row r
+  while (lo < hi) {
+    const int n = hi - lo, p = n <= 64 ? min(lo + lane, hi - 1) : lo + (int)((int64_t)n * (lane + 1) / 65);
+    const int below = __popcll(__ballot(s[p].y < (uint32_t)r));
+    const int from = lo;
+    if (n <= 64) {
+      lo = hi = from + min(below, n);
+    } else {
+      if (below) lo = from + (int)((int64_t)n * below / 65) + 1;
+      if (below < 64) hi = from + (int)((int64_t)n * (below + 1) / 65);
     }
+  }
+  const float* parts = c.parts + 2 * id * c.pieces * c.dim;
+  for (int col = 4 * lane; col < c.dim; col += 256) {
+    const int n = min(4, c.dim - col);
+    float sum[4] = {0.f, 0.f, 0.f, 0.f}, e[4];
+#pragma unroll 16
+    for (int64_t q = (lo + r) / c.items; q < piece; ++q) {
+      load4(parts + (2 * q + 1) * c.dim + col, n, e);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) sum[v] += e[v];
+    }
+    load4(parts + 2 * piece * c.dim + col, n, e);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) sum[v] = c.scale * (sum[v] + e[v]);
+    store4(c.G + id * c.ld + (int64_t)r * c.dim + col, n, sum);
   }
 }
 
@@ -372,6 +371,8 @@ void embed_grad_launch(const void* dY, const int32_t* tokens, GradCall c, const 
   c.items = w.items;
   int bits = 1;
   while ((c.vocab + 1) >> bits) ++bits;  // of vocab + 1, the largest key
+  // one run up to 8,192 tokens: 18 us at that length, against 8 us for runs of 2,048 and 14 to
+  // join them
   int run = kSortThreads;
   if (!c.T) {
     // no tokens to sort
@@ -394,7 +395,7 @@ void embed_grad_launch(const void* dY, const int32_t* tokens, GradCall c, const 
   while (c.L < 128 && c.L * 4 < c.dim) c.L *= 2;
   hipLaunchKernelGGL(k_embed_grad<T>, dim3((unsigned)ceil_div(c.pieces, 256 / c.L), c.groups.count), dim3(256),
                      0, s, static_cast<const T*>(dY), c);
-  hipLaunchKernelGGL(k_embed_join, dim3((unsigned)ceil_div(c.pieces, kJoinPieces), c.groups.count), dim3(256), 0, s, c);
+  hipLaunchKernelGGL(k_embed_join, dim3((unsigned)ceil_div(c.pieces, 4), c.groups.count), dim3(256), 0, s, c);
 }
 
 }  // namespace
