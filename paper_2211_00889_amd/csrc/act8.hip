@@ -25,62 +25,129 @@ __device__ __forceinline__ uint32_t step_byte(float peak) {
   return (uint32_t)(min(max(k, -126), 121) + 127);
 }
 
-// A thread a channel and block of 32 tokens.
+// Packing and unpacking are copies with a transposition of 32 tokens: what bounds them is HBM.
+// A thread takes V channels (8 bytes of a row in bf16, 16 in fp32) and 8 of a block's 32 tokens, four
+// threads a block; the four put their part of the peaks together by shuffles, and each has
+// 8 consecutive bytes of a channel, so that a wave writes 16 V x 32 contiguous bytes.  A
+// thread with a channel's whole block (64 bytes a wave of a bf16 row) ran at 2.3 TB/s.
+template <typename T>
+struct PackTile {
+  static constexpr int V = 4, CH = 16 * V;  // channels of a wave
+};
+
+// The V elements at p, the first n of them; zeros behind.
+__device__ __forceinline__ void load_v(const float* p, int n, float (&v)[4]) {
+  Elem<float>::expand(load16<float>(p, n), v);
+}
+__device__ __forceinline__ void load_v(const __bf16* p, int n, float (&v)[4]) {
+  if (n >= 4) {
+    const u32x2 r = *reinterpret_cast<const u32x2_any*>(p);
+    v[0] = bf16_lo(r[0]), v[1] = bf16_hi(r[0]), v[2] = bf16_lo(r[1]), v[3] = bf16_hi(r[1]);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = k < n ? (float)p[k] : 0.f;
+}
+__device__ __forceinline__ void store_v(float* p, int n, const float (&v)[4]) {
+  store16<float>(p, Elem<float>::collapse(v), n);
+}
+__device__ __forceinline__ void store_v(__bf16* p, int n, const float (&v)[4]) {
+  if (n >= 4) {
+    *reinterpret_cast<u32x2_any*>(p) = (u32x2){pack2(v[0], v[1]), pack2(v[2], v[3])};
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (k < n) p[k] = (__bf16)v[k];
+}
+
+// Lane: channels V (lane / 4) of the wave's, tokens 8 (lane % 4) of the block.
 template <typename T>
 __global__ void __launch_bounds__(256)
     k_act8_pack(const T* __restrict__ A, int64_t lda, int Tn, int dim, uint8_t* __restrict__ packed,
                 Act8 lay, Groups groups) {
-  const int ch = blockIdx.x * 256 + threadIdx.x;
-  if (ch >= dim) return;
+  constexpr int V = PackTile<T>::V, CH = PackTile<T>::CH;
+  const int lane = threadIdx.x & 63, oct = lane & 3;
+  const int ch = (blockIdx.x * 4 + (threadIdx.x >> 6)) * CH + (lane >> 2) * V;
+  const int n = dim - ch;
   const int64_t blk = blockIdx.y;
   const int64_t id = group_id(groups, blockIdx.z);
-  const int t0 = (int)blk * kActBlock, live = min(kActBlock, Tn - t0);
+  const int t0 = (int)blk * kActBlock + 8 * oct;
   const T* src = A + (id * Tn + t0) * lda + ch;
-  float v[kActBlock];
-  uint32_t peak = 0;  // as bits: a NaN stays the largest
+  float v[8][V];
+  uint32_t peak[V];  // as bits: a NaN stays the largest
 #pragma unroll
-  for (int t = 0; t < kActBlock; ++t) {
-    v[t] = t < live ? Elem<T>::load(src + t * lda) : 0.f;
-    peak = max(peak, __builtin_bit_cast(uint32_t, v[t]) & 0x7fffffffu);
-  }
-  const uint32_t byte = step_byte(__builtin_bit_cast(float, peak));
-  const float inv = byte == 255u ? 0.f : __builtin_bit_cast(float, (254u - byte) << 23);
-  uint8_t* base = packed + id * lay.bytes;
-  uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (byte != 255u) {
+  for (int k = 0; k < V; ++k) peak[k] = 0u;
 #pragma unroll
-    for (int t = 0; t < kActBlock; ++t) {
-      const int q = (int)fminf(fmaxf(rintf(v[t] * inv), -127.f), 127.f);
-      w[t >> 2] |= ((uint32_t)q & 0xffu) << (8 * (t & 3));
+  for (int t = 0; t < 8; ++t) {
+    if (n > 0 && t0 + t < Tn) {
+      load_v(src + t * lda, n, v[t]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[t][k] = 0.f;
     }
   }
-  u32x4* dst = reinterpret_cast<u32x4*>(base + (blk * dim + ch) * kActBlock);
-  dst[0] = (u32x4){w[0], w[1], w[2], w[3]};
-  dst[1] = (u32x4){w[4], w[5], w[6], w[7]};
-  uint8_t* steps = base + lay.scale + ((blk >> 2) * dim + ch) * 4;
-  steps[blk & 3] = (uint8_t)byte;
-  if (blk == lay.blocks - 1)  // the rest of the last four
-    for (int k = (int)(blk & 3) + 1; k < 4; ++k) steps[k] = 0;
+#pragma unroll
+  for (int t = 0; t < 8; ++t)
+#pragma unroll
+    for (int k = 0; k < V; ++k) peak[k] = max(peak[k], __builtin_bit_cast(uint32_t, v[t][k]) & 0x7fffffffu);
+  uint8_t* base = packed + id * lay.bytes;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    peak[k] = max(peak[k], (uint32_t)__shfl_xor((int)peak[k], 1));
+    peak[k] = max(peak[k], (uint32_t)__shfl_xor((int)peak[k], 2));
+    const uint32_t byte = step_byte(__builtin_bit_cast(float, peak[k]));
+    const float inv = byte == 255u ? 0.f : __builtin_bit_cast(float, (254u - byte) << 23);
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      // a NaN's conversion is 0, an infinity times 0 is one
+      const int q = (int)fminf(fmaxf(rintf(v[t][k] * inv), -127.f), 127.f);
+      w[t >> 2] |= ((uint32_t)q & 0xffu) << (8 * (t & 3));
+    }
+    if (byte == 255u) w[0] = w[1] = 0u;
+    if (k < n) {
+      *reinterpret_cast<u32x2*>(base + (blk * dim + ch + k) * kActBlock + 8 * oct) = (u32x2){w[0], w[1]};
+      if (oct == 0) {
+        uint8_t* steps = base + lay.scale + ((blk >> 2) * dim + ch + k) * 4;
+        steps[blk & 3] = (uint8_t)byte;
+        if (blk == lay.blocks - 1)  // the rest of the last four
+          for (int r = (int)(blk & 3) + 1; r < 4; ++r) steps[r] = 0;
+      }
+    }
+  }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(256)
     k_act8_unpack(const uint8_t* __restrict__ packed, int Tn, int dim, T* __restrict__ A, int64_t lda,
                   Act8 lay, Groups groups) {
-  const int ch = blockIdx.x * 256 + threadIdx.x;
-  if (ch >= dim) return;
+  constexpr int V = PackTile<T>::V, CH = PackTile<T>::CH;
+  const int lane = threadIdx.x & 63, oct = lane & 3;
+  const int ch = (blockIdx.x * 4 + (threadIdx.x >> 6)) * CH + (lane >> 2) * V;
+  const int n = dim - ch;
+  if (n <= 0) return;
   const int64_t blk = blockIdx.y;
   const int64_t id = group_id(groups, blockIdx.z);
-  const int t0 = (int)blk * kActBlock, live = min(kActBlock, Tn - t0);
+  const int t0 = (int)blk * kActBlock + 8 * oct;
   const uint8_t* base = packed + id * lay.bytes;
-  const u32x4* src = reinterpret_cast<const u32x4*>(base + (blk * dim + ch) * kActBlock);
-  const u32x4 w[2] = {src[0], src[1]};
-  const float step = step_of(base[lay.scale + ((blk >> 2) * dim + ch) * 4 + (blk & 3)]);
+  u32x2 q[V];
+  float step[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    const int64_t c = min(ch + k, dim - 1);
+    q[k] = *reinterpret_cast<const u32x2*>(base + (blk * dim + c) * kActBlock + 8 * oct);
+    step[k] = step_of(base[lay.scale + ((blk >> 2) * dim + c) * 4 + (blk & 3)]);
+  }
   T* dst = A + (id * Tn + t0) * lda + ch;
 #pragma unroll
-  for (int t = 0; t < kActBlock; ++t)
-    if (t < live)
-      Elem<T>::store(dst + t * lda, step * (float)(int8_t)(w[t >> 4][(t >> 2) & 3] >> (8 * (t & 3))));
+  for (int t = 0; t < 8; ++t) {
+    if (t0 + t >= Tn) break;
+    float v[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = step[k] * (float)(int8_t)(q[k][t >> 2] >> (8 * (t & 3)));
+    store_v(dst + t * lda, n, v);
+  }
 }
 
 // Weight gradient dW = A^T dY: the tokens are the K of MFMA 16x16x32 (bf16, fp32 sums), a
@@ -315,7 +382,7 @@ template <typename T>
 nbsgd_status pack_launch(const void* A, int64_t lda, int32_t Tn, int32_t dim, void* packed,
                          const Groups& g, hipStream_t s) {
   const Act8 lay = act8_layout(Tn, dim);
-  const dim3 grid((unsigned)ceil_div(dim, 256), (unsigned)lay.blocks, g.count);
+  const dim3 grid((unsigned)ceil_div(dim, 4 * PackTile<T>::CH), (unsigned)lay.blocks, g.count);
   hipLaunchKernelGGL(k_act8_pack<T>, grid, dim3(256), 0, s, static_cast<const T*>(A), lda, Tn, dim,
                      static_cast<uint8_t*>(packed), lay, g);
   return launched("nbsgd_act_pack");
@@ -325,7 +392,7 @@ template <typename T>
 nbsgd_status unpack_launch(const void* packed, int32_t Tn, int32_t dim, void* A, int64_t lda,
                            const Groups& g, hipStream_t s) {
   const Act8 lay = act8_layout(Tn, dim);
-  const dim3 grid((unsigned)ceil_div(dim, 256), (unsigned)lay.blocks, g.count);
+  const dim3 grid((unsigned)ceil_div(dim, 4 * PackTile<T>::CH), (unsigned)lay.blocks, g.count);
   hipLaunchKernelGGL(k_act8_unpack<T>, grid, dim3(256), 0, s, static_cast<const uint8_t*>(packed), Tn,
                      dim, static_cast<T*>(A), lda, lay, g);
   return launched("nbsgd_act_unpack");
