@@ -29,7 +29,8 @@ __device__ __forceinline__ uint32_t step_byte(float peak) {
 // A thread takes V channels (8 bytes of a row in bf16, 16 in fp32) and 8 of a block's 32 tokens, four
 // threads a block; the four put their part of the peaks together by shuffles, and each has
 // 8 consecutive bytes of a channel, so that a wave writes 16 V x 32 contiguous bytes.  A
-// thread with a channel's whole block (64 bytes a wave of a bf16 row) ran at 2.3 TB/s.
+// thread with a channel's whole block (128 bytes a load of bf16) packed at 2.3 TB/s.  It goes on
+// to the next of four blocks, whose steps make one word.
 template <typename T>
 struct PackTile {
   static constexpr int V = 4, CH = 16 * V;  // channels of a wave
@@ -61,7 +62,24 @@ __device__ __forceinline__ void store_v(__bf16* p, int n, const float (&v)[4]) {
     if (k < n) p[k] = (__bf16)v[k];
 }
 
-// Lane: channels V (lane / 4) of the wave's, tokens 8 (lane % 4) of the block.
+// The value of the lane whose number differs in bit D (0 or 1), within four lanes.
+template <int D>
+__device__ __forceinline__ uint32_t swap_lane(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, D ? 0x4e : 0xb1, 0xf, 0xf, true);
+}
+// a of the lanes with bit D against b of those without it.
+template <int D>
+__device__ __forceinline__ void exchange(int lane, u32x2& a, u32x2& b) {
+  const bool up = lane >> D & 1;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t got = swap_lane<D>(up ? a[h] : b[h]);
+    if (up) a[h] = got;
+    else b[h] = got;
+  }
+}
+
+// Lane: channels V (lane / 4) of the wave's, tokens 8 (lane % 4) of each of four blocks.
 template <typename T>
 __global__ void __launch_bounds__(256)
     k_act8_pack(const T* __restrict__ A, int64_t lda, int Tn, int dim, uint8_t* __restrict__ packed,
@@ -70,51 +88,66 @@ __global__ void __launch_bounds__(256)
   const int lane = threadIdx.x & 63, oct = lane & 3;
   const int ch = (blockIdx.x * 4 + (threadIdx.x >> 6)) * CH + (lane >> 2) * V;
   const int n = dim - ch;
-  const int64_t blk = blockIdx.y;
   const int64_t id = group_id(groups, blockIdx.z);
-  const int t0 = (int)blk * kActBlock + 8 * oct;
-  const T* src = A + (id * Tn + t0) * lda + ch;
-  float v[8][V];
-  uint32_t peak[V];  // as bits: a NaN stays the largest
-#pragma unroll
-  for (int k = 0; k < V; ++k) peak[k] = 0u;
-#pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    if (n > 0 && t0 + t < Tn) {
-      load_v(src + t * lda, n, v[t]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < V; ++k) v[t][k] = 0.f;
-    }
-  }
-#pragma unroll
-  for (int t = 0; t < 8; ++t)
-#pragma unroll
-    for (int k = 0; k < V; ++k) peak[k] = max(peak[k], __builtin_bit_cast(uint32_t, v[t][k]) & 0x7fffffffu);
+  const T* src = A + id * Tn * lda + ch;
   uint8_t* base = packed + id * lay.bytes;
+  const int64_t blk0 = 4 * (int64_t)blockIdx.y;
+  uint32_t steps[V];
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-    peak[k] = max(peak[k], (uint32_t)__shfl_xor((int)peak[k], 1));
-    peak[k] = max(peak[k], (uint32_t)__shfl_xor((int)peak[k], 2));
-    const uint32_t byte = step_byte(__builtin_bit_cast(float, peak[k]));
-    const float inv = byte == 255u ? 0.f : __builtin_bit_cast(float, (254u - byte) << 23);
-    uint32_t w[2] = {0u, 0u};
+  for (int k = 0; k < V; ++k) steps[k] = 0u;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    if (blk0 + b >= lay.blocks) break;  // uniform
+    const int t0 = (int)(blk0 + b) * kActBlock + 8 * oct;
+    float v[8][V];
+    uint32_t peak[V];  // as bits: a NaN stays the largest
+#pragma unroll
+    for (int k = 0; k < V; ++k) peak[k] = 0u;
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
-      // a NaN's conversion is 0, an infinity times 0 is one
-      const int q = (int)fminf(fmaxf(rintf(v[t][k] * inv), -127.f), 127.f);
-      w[t >> 2] |= ((uint32_t)q & 0xffu) << (8 * (t & 3));
-    }
-    if (byte == 255u) w[0] = w[1] = 0u;
-    if (k < n) {
-      *reinterpret_cast<u32x2*>(base + (blk * dim + ch + k) * kActBlock + 8 * oct) = (u32x2){w[0], w[1]};
-      if (oct == 0) {
-        uint8_t* steps = base + lay.scale + ((blk >> 2) * dim + ch + k) * 4;
-        steps[blk & 3] = (uint8_t)byte;
-        if (blk == lay.blocks - 1)  // the rest of the last four
-          for (int r = (int)(blk & 3) + 1; r < 4; ++r) steps[r] = 0;
+      if (n > 0 && t0 + t < Tn) {
+        load_v(src + (int64_t)(t0 + t) * lda, n, v[t]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[t][k] = 0.f;
       }
     }
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+#pragma unroll
+      for (int k = 0; k < V; ++k) peak[k] = max(peak[k], __builtin_bit_cast(uint32_t, v[t][k]) & 0x7fffffffu);
+    u32x2 out[V];  // this lane's 8 tokens of its four channels
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      peak[k] = max(peak[k], swap_lane<0>(peak[k]));
+      peak[k] = max(peak[k], swap_lane<1>(peak[k]));
+      const uint32_t byte = step_byte(__builtin_bit_cast(float, peak[k]));
+      steps[k] |= byte << (8 * b);
+      const float inv = byte == 255u ? 0.f : __builtin_bit_cast(float, (254u - byte) << 23);
+      uint32_t w[2] = {0u, 0u};
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int q = (int)fminf(fmaxf(rintf(v[t][k] * inv), -127.f), 127.f);
+        w[t >> 2] |= ((uint32_t)q & 0xffu) << (8 * (t & 3));
+      }
+      out[k] = byte == 255u ? (u32x2){0u, 0u} : (u32x2){w[0], w[1]};
+    }
+    // four lanes turn their 4 x 4 parts, so that each has the 32 tokens of one channel
+    exchange<0>(lane, out[0], out[1]);
+    exchange<0>(lane, out[2], out[3]);
+    exchange<1>(lane, out[0], out[2]);
+    exchange<1>(lane, out[1], out[3]);
+    if (oct < n) {
+      u32x4* to = reinterpret_cast<u32x4*>(base + ((blk0 + b) * dim + ch + oct) * kActBlock);
+      to[0] = (u32x4){out[0][0], out[0][1], out[1][0], out[1][1]};
+      to[1] = (u32x4){out[2][0], out[2][1], out[3][0], out[3][1]};
+    }
+  }
+  if (oct == 0) {
+    uint32_t* to = reinterpret_cast<uint32_t*>(base + lay.scale) + (int64_t)blockIdx.y * dim + ch;
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (k < n) to[k] = steps[k];
   }
 }
 
@@ -127,26 +160,31 @@ __global__ void __launch_bounds__(256)
   const int ch = (blockIdx.x * 4 + (threadIdx.x >> 6)) * CH + (lane >> 2) * V;
   const int n = dim - ch;
   if (n <= 0) return;
-  const int64_t blk = blockIdx.y;
   const int64_t id = group_id(groups, blockIdx.z);
-  const int t0 = (int)blk * kActBlock + 8 * oct;
   const uint8_t* base = packed + id * lay.bytes;
-  u32x2 q[V];
-  float step[V];
+  const uint32_t* from = reinterpret_cast<const uint32_t*>(base + lay.scale) + (int64_t)blockIdx.y * dim;
+  const int64_t blk0 = 4 * (int64_t)blockIdx.y;
+  uint32_t steps[V];
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-    const int64_t c = min(ch + k, dim - 1);
-    q[k] = *reinterpret_cast<const u32x2*>(base + (blk * dim + c) * kActBlock + 8 * oct);
-    step[k] = step_of(base[lay.scale + ((blk >> 2) * dim + c) * 4 + (blk & 3)]);
-  }
-  T* dst = A + (id * Tn + t0) * lda + ch;
+  for (int k = 0; k < V; ++k) steps[k] = from[min(ch + k, dim - 1)];
+  T* dst = A + id * Tn * lda + ch;
 #pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    if (t0 + t >= Tn) break;
-    float v[V];
+  for (int b = 0; b < 4; ++b) {
+    if (blk0 + b >= lay.blocks) break;  // uniform
+    const int t0 = (int)(blk0 + b) * kActBlock + 8 * oct;
+    u32x2 q[V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = step[k] * (float)(int8_t)(q[k][t >> 2] >> (8 * (t & 3)));
-    store_v(dst + t * lda, n, v);
+    for (int k = 0; k < V; ++k)
+      q[k] = *reinterpret_cast<const u32x2*>(base + ((blk0 + b) * dim + min(ch + k, dim - 1)) * kActBlock + 8 * oct);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      if (t0 + t >= Tn) break;
+      float v[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        v[k] = step_of(steps[k] >> (8 * b) & 0xffu) * (float)(int8_t)(q[k][t >> 2] >> (8 * (t & 3)));
+      store_v(dst + (int64_t)(t0 + t) * lda, n, v);
+    }
   }
 }
 
@@ -382,7 +420,7 @@ template <typename T>
 nbsgd_status pack_launch(const void* A, int64_t lda, int32_t Tn, int32_t dim, void* packed,
                          const Groups& g, hipStream_t s) {
   const Act8 lay = act8_layout(Tn, dim);
-  const dim3 grid((unsigned)ceil_div(dim, 4 * PackTile<T>::CH), (unsigned)lay.blocks, g.count);
+  const dim3 grid((unsigned)ceil_div(dim, 4 * PackTile<T>::CH), (unsigned)ceil_div(lay.blocks, 4), g.count);
   hipLaunchKernelGGL(k_act8_pack<T>, grid, dim3(256), 0, s, static_cast<const T*>(A), lda, Tn, dim,
                      static_cast<uint8_t*>(packed), lay, g);
   return launched("nbsgd_act_pack");
@@ -392,7 +430,7 @@ template <typename T>
 nbsgd_status unpack_launch(const void* packed, int32_t Tn, int32_t dim, void* A, int64_t lda,
                            const Groups& g, hipStream_t s) {
   const Act8 lay = act8_layout(Tn, dim);
-  const dim3 grid((unsigned)ceil_div(dim, 4 * PackTile<T>::CH), (unsigned)lay.blocks, g.count);
+  const dim3 grid((unsigned)ceil_div(dim, 4 * PackTile<T>::CH), (unsigned)ceil_div(lay.blocks, 4), g.count);
   hipLaunchKernelGGL(k_act8_unpack<T>, grid, dim3(256), 0, s, static_cast<const uint8_t*>(packed), Tn,
                      dim, static_cast<T*>(A), lda, lay, g);
   return launched("nbsgd_act_unpack");
