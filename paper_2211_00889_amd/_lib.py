@@ -465,24 +465,29 @@ def mlp_loss(params, dims, data, labels, idx, losses, workspace, stream=None):
 
 
 # ------------------------------------------------------------ token models
-def _rows(t, name, lead, width=None, like=None):
-    """(pointer, row stride, dtype) of activations [*lead, width]: float32 or bfloat16 rows, a
-    constant number of elements apart in the order of the leading dimensions."""
+# A served token's kernel takes 3 us, so these calls are bound by the host: a tensor is looked at
+# once, contiguous ones without a walk over their strides, and devices are compared as numbers
+# (nbsgd_scan's marshalling took 8.6 us with lists of tensors and torch.device objects).
+def _rows(t, name, shape, like=None):
+    """(pointer, row stride, dtype) of activations of this shape, [..., width]: float32 or bfloat16
+    rows, a constant number of elements apart in the order of the leading dimensions."""
     torch = _torch or _use_torch()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    dtype = F32 if t.dtype == torch.float32 else BF16 if t.dtype == torch.bfloat16 else None
-    if dtype is None or (like is not None and t.dtype != like.dtype):
+    dt = t.dtype
+    if (dt is not torch.float32 and dt is not torch.bfloat16) or (like is not None and dt is not like):
         raise TypeError(f"{name} must be float32 or bfloat16" + (", as the other rows" if like is not None else ""))
-    if t.dim() != len(lead) + 1 or tuple(t.shape[:-1]) != lead or (width is not None and t.shape[-1] != width):
-        raise ValueError(f"{name} must be {list(lead) + [width if width is not None else 'width']}")
-    shape, strides = t.shape, t.stride()
-    if shape[-1] > 1 and strides[-1] != 1:
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}")
+    code = F32 if dt is torch.float32 else BF16
+    width = shape[-1]
+    if t.is_contiguous() or not t.numel():
+        return t.data_ptr(), width, code
+    strides = t.stride()
+    if width > 1 and strides[-1] != 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
-    if not t.numel():
-        return t.data_ptr(), shape[-1], dtype
     ld = rows = None
-    for k in range(len(lead) - 1, -1, -1):  # dimensions of one entry have no stride of their own
+    for k in range(len(shape) - 2, -1, -1):  # dimensions of one entry have no stride of their own
         if shape[k] != 1:
             if ld is None:
                 ld, rows = strides[k], shape[k]
@@ -490,17 +495,16 @@ def _rows(t, name, lead, width=None, like=None):
                 raise ValueError(f"{name}: the rows must lie a constant stride apart")
             else:
                 rows *= shape[k]
-    return t.data_ptr(), shape[-1] if ld is None else ld, dtype
+    return t.data_ptr(), width if ld is None else ld, code
 
 
 def _whole(t, name, dtype, shape):
     """Pointer of a contiguous device tensor of this type and shape; None stays null."""
     if t is None:
         return None
-    torch = _torch or _use_torch()
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+    if not isinstance(t, (_torch or _use_torch()).Tensor) or not t.is_cuda or t.dtype is not dtype or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}")
     return t.data_ptr()
 
@@ -508,32 +512,28 @@ def _whole(t, name, dtype, shape):
 def _params(t, name, lead, offset, count):
     """(pointer, row stride) of `count` parameters at `offset` of every row of X or G."""
     torch = _torch or _use_torch()
-    if t.dim() != len(lead) + 1 or tuple(t.shape[:-1]) != lead:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.float32 or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous torch.float32 CUDA tensor")
+    shape = t.shape
+    if shape[:-1] != lead or len(shape) != len(lead) + 1:
         raise ValueError(f"{name} must be {list(lead) + ['row']}")
-    ld = t.shape[-1]
+    ld = shape[-1]
     if offset < 0 or offset + count > ld:
         raise ValueError(f"{name}: {count} floats at {offset} do not fit rows of {ld}")
-    return _whole(t, name, torch.float32, t.shape) + 4 * offset, ld
+    return t.data_ptr() + 4 * offset, ld
 
 
-class _On:
-    """The call's device: every tensor is on one, which is made the current one for the call."""
-
-    def __init__(self, *tensors):
-        torch = _torch or _use_torch()
-        device = tensors[0].device
-        for t in tensors[1:]:
-            if t is not None and t.device != device:
-                raise ValueError(f"tensors on {device} and {t.device}")
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _call(fn, stream, lead, tensors, args):
+    """The library's call on the tensors' device, which is made the current one for it."""
+    torch = _torch or _use_torch()
+    index = lead.get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"tensors on {lead.device} and {t.device}")
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return _check(fn(*args, _stream(lead, stream)))
+    _check(fn(*args, _stream(lead, stream)))
 
 
 def _workspace(t):
@@ -544,15 +544,13 @@ def embed(X, offset: int, vocab: int, tokens, mask, Y, scale: float = 1.0, strea
     """Y[i, j, t] = scale * E_i[tokens[i, j, t]], the table E_i [vocab, dim] at ``offset`` of row i
     of X [n, ld]; tokens int32 [n, m, T], Y [n, m, T, dim] float32 or bfloat16 rows.  Tokens
     outside [0, vocab) give zeros; unfinished mini-batches (mask [n, m]) are left alone."""
-    n, m, T = tokens.shape
     torch = _torch or _use_torch()
-    y, ldy, dtype = _rows(Y, "Y", (n, m, T))
-    dim = Y.shape[-1]
+    n, m, T, dim = shape = Y.shape
+    y, ldy, dtype = _rows(Y, "Y", shape)
     e, ld = _params(X, "X", (n,), offset, vocab * dim)
     tok = _whole(tokens, "tokens", torch.int32, (n, m, T))
-    with _On(X, tokens, Y):
-        _check(load().nbsgd_embed(e, ld, n, m, vocab, dim, scale, tok, T, _u8(mask, (n, m)), y, ldy, dtype,
-                                  _stream(X, stream)))
+    _call(load().nbsgd_embed, stream, X, (tokens, Y),
+          (e, ld, n, m, vocab, dim, scale, tok, T, _u8(mask, (n, m)), y, ldy, dtype))
 
 
 def embed_workspace_bytes(n: int, m: int, T: int, vocab: int, dim: int) -> int:
@@ -564,16 +562,14 @@ def embed_workspace_bytes(n: int, m: int, T: int, vocab: int, dim: int) -> int:
 def embed_grad(dY, tokens, mask, G, offset: int, vocab: int, workspace, scale: float = 1.0, stream=None):
     """The table's gradient, scale * the sum of a token's rows of dY [n, m, T, dim], every row of
     the table, at ``offset`` of the rows of G [n, m, ld]."""
-    n, m, T = tokens.shape
     torch = _torch or _use_torch()
-    d, ldy, dtype = _rows(dY, "dY", (n, m, T))
-    dim = dY.shape[-1]
+    n, m, T, dim = shape = dY.shape
+    d, ldy, dtype = _rows(dY, "dY", shape)
     g, ld = _params(G, "G", (n, m), offset, vocab * dim)
     tok = _whole(tokens, "tokens", torch.int32, (n, m, T))
     ws, ws_bytes = _workspace(workspace)
-    with _On(G, tokens, dY, workspace):
-        _check(load().nbsgd_embed_grad(d, ldy, dtype, n, m, T, tok, vocab, dim, scale, _u8(mask, (n, m)), g,
-                                       ld, ws, ws_bytes, _stream(G, stream)))
+    _call(load().nbsgd_embed_grad, stream, G, (tokens, dY, workspace),
+          (d, ldy, dtype, n, m, T, tok, vocab, dim, scale, _u8(mask, (n, m)), g, ld, ws, ws_bytes))
 
 
 def scan_workspace_bytes(n: int, m: int, batch: int, T: int, dim: int) -> int:
@@ -584,17 +580,15 @@ def scan_workspace_bytes(n: int, m: int, batch: int, T: int, dim: int) -> int:
 
 def _scan_args(x, g, X, offset, lengths, states):
     torch = _torch or _use_torch()
-    n, m, b, T, dim = x.shape
-    lead = (n, m, b, T)
-    px, ldx, dtype = _rows(x, "x", lead)
-    pg, ldg, _ = _rows(g, "g", lead, dim, x)
+    n, m, b, T, dim = shape = x.shape
+    px, ldx, dtype = _rows(x, "x", shape)
+    pg, ldg, _ = _rows(g, "g", shape, x.dtype)
     if ldg != ldx:
         raise ValueError("x and g must have one row stride")
     bias, ld = (None, dim) if X is None else _params(X, "X", (n,), offset, dim)
-    f32 = torch.float32
-    return (lead, dim, px, pg, ldx, dtype, bias, ld,
+    return (px, pg, ldx, dtype, n, m, b, T, dim, bias, ld,
             _whole(lengths, "lengths", torch.int32, (n, m, b)),
-            _whole(states, "states", f32, (n, m, b, -(-T // SCAN_INTERVAL), dim)))
+            _whole(states, "states", torch.float32, (n, m, b, -(-T // SCAN_INTERVAL), dim)))
 
 
 def scan(x, g, mask, h, X=None, offset: int = 0, h0=None, h_last=None, lengths=None, states=None,
@@ -603,30 +597,28 @@ def scan(x, g, mask, h, X=None, offset: int = 0, h0=None, h_last=None, lengths=N
     [n, m, batch, T, dim] (float32 or bfloat16 rows); the bias [dim] at ``offset`` of row i of
     X [n, ld], or none.  h0 and h_last float32 [n, m, batch, dim] (h_last may be h0), lengths int32
     [n, m, batch], states float32 [n, m, batch, ceil(T / SCAN_INTERVAL), dim] for the backward pass."""
-    torch = _torch or _use_torch()
-    (lead, dim, px, pg, ldx, dtype, bias, ld, lens, st) = _scan_args(x, g, X, offset, lengths, states)
-    ph, ldh, _ = _rows(h, "h", lead, dim, x)
-    n, m, b, T = lead
-    f32 = torch.float32
+    f32 = (_torch or _use_torch()).float32
+    *args, lens, st = _scan_args(x, g, X, offset, lengths, states)
+    n, m, b, T, dim = shape = x.shape
+    ph, ldh, _ = _rows(h, "h", shape, x.dtype)
+    kept = (n, m, b, dim)
     ws, ws_bytes = _workspace(workspace)
-    with _On(x, g, h, X, h0, h_last, lengths, states, workspace):
-        _check(load().nbsgd_scan(px, pg, ldx, dtype, n, m, b, T, dim, bias, ld, lens, _u8(mask, (n, m)),
-                                 _whole(h0, "h0", f32, (n, m, b, dim)), ph, ldh,
-                                 _whole(h_last, "h_last", f32, (n, m, b, dim)), st, ws, ws_bytes,
-                                 _stream(x, stream)))
+    _call(load().nbsgd_scan, stream, x, (g, h, X, h0, h_last, lengths, states, workspace),
+          (*args, lens, _u8(mask, (n, m)), _whole(h0, "h0", f32, kept), ph, ldh,
+           _whole(h_last, "h_last", f32, kept), st, ws, ws_bytes))
 
 
 def scan_grad(x, g, states, dh, mask, dx, dg, workspace, X=None, G=None, offset: int = 0, dh_last=None,
               dh0=None, lengths=None, stream=None):
     """The backward pass of ``scan``: dx and dg laid out as x and g, dh0 [n, m, batch, dim], and the
     bias's gradient at ``offset`` of the rows of G [n, m, ld]; X and G have one row stride."""
-    torch = _torch or _use_torch()
-    (lead, dim, px, pg, ldx, dtype, bias, ld, lens, st) = _scan_args(x, g, X, offset, lengths, states)
-    pd, lddh, _ = _rows(dh, "dh", lead, dim, x)
-    pdx, lddx, _ = _rows(dx, "dx", lead, dim, x)
-    pdg, lddg, _ = _rows(dg, "dg", lead, dim, x)
-    n, m, b, T = lead
-    if x.numel() and (lddx != ldx or lddg != ldx):
+    f32 = (_torch or _use_torch()).float32
+    px, pg, ldx, dtype, n, m, b, T, dim, bias, ld, lens, st = _scan_args(x, g, X, offset, lengths, states)
+    shape, dt = x.shape, x.dtype
+    pd, lddh, _ = _rows(dh, "dh", shape, dt)
+    pdx, lddx, _ = _rows(dx, "dx", shape, dt)
+    pdg, lddg, _ = _rows(dg, "dg", shape, dt)
+    if lddx != ldx or lddg != ldx:
         raise ValueError("dx and dg must have the row stride of x and g")
     gb = None
     if G is not None:
@@ -634,13 +626,11 @@ def scan_grad(x, g, states, dh, mask, dx, dg, workspace, X=None, G=None, offset:
         if X is not None and ldg != ld:
             raise ValueError("X and G must have one row stride")
         ld = ldg
-    f32 = torch.float32
+    kept = (n, m, b, dim)
     ws, ws_bytes = _workspace(workspace)
-    with _On(x, g, states, dh, dx, dg, X, G, dh_last, dh0, lengths, workspace):
-        _check(load().nbsgd_scan_grad(px, pg, ldx, dtype, n, m, b, T, dim, bias, ld, lens, _u8(mask, (n, m)),
-                                      st, pd, lddh, _whole(dh_last, "dh_last", f32, (n, m, b, dim)), pdx,
-                                      pdg, _whole(dh0, "dh0", f32, (n, m, b, dim)), gb, ws, ws_bytes,
-                                      _stream(x, stream)))
+    _call(load().nbsgd_scan_grad, stream, x, (g, states, dh, dx, dg, X, G, dh_last, dh0, lengths, workspace),
+          (px, pg, ldx, dtype, n, m, b, T, dim, bias, ld, lens, _u8(mask, (n, m)), st, pd, lddh,
+           _whole(dh_last, "dh_last", f32, kept), pdx, pdg, _whole(dh0, "dh0", f32, kept), gb, ws, ws_bytes))
 
 
 def act_bytes(T: int, dim: int) -> int:
@@ -651,26 +641,23 @@ def act_bytes(T: int, dim: int) -> int:
 
 
 def _packed(t, n, m, T, dim):
-    torch = _torch or _use_torch()
-    return _whole(t, "packed", torch.uint8, (n, m, act_bytes(T, dim)))
+    return _whole(t, "packed", (_torch or _use_torch()).uint8, (n, m, act_bytes(T, dim)))
 
 
 def act_pack(A, mask, packed, stream=None):
     """A [n, m, T, dim] (float32 or bfloat16 rows) into packed uint8 [n, m, act_bytes(T, dim)]."""
-    n, m, T, dim = A.shape
-    a, lda, dtype = _rows(A, "A", (n, m, T))
-    with _On(A, packed):
-        _check(load().nbsgd_act_pack(a, lda, dtype, n, m, T, dim, _u8(mask, (n, m)),
-                                      _packed(packed, n, m, T, dim), _stream(A, stream)))
+    n, m, T, dim = shape = A.shape
+    a, lda, dtype = _rows(A, "A", shape)
+    _call(load().nbsgd_act_pack, stream, A, (packed,),
+          (a, lda, dtype, n, m, T, dim, _u8(mask, (n, m)), _packed(packed, n, m, T, dim)))
 
 
 def act_unpack(packed, mask, A, stream=None):
     """The values that packed stands for, into A [n, m, T, dim]."""
-    n, m, T, dim = A.shape
-    a, lda, dtype = _rows(A, "A", (n, m, T))
-    with _On(A, packed):
-        _check(load().nbsgd_act_unpack(_packed(packed, n, m, T, dim), n, m, T, dim, _u8(mask, (n, m)), a,
-                                        lda, dtype, _stream(A, stream)))
+    n, m, T, dim = shape = A.shape
+    a, lda, dtype = _rows(A, "A", shape)
+    _call(load().nbsgd_act_unpack, stream, A, (packed,),
+          (_packed(packed, n, m, T, dim), n, m, T, dim, _u8(mask, (n, m)), a, lda, dtype))
 
 
 def act_workspace_bytes(n: int, m: int, T: int, dim: int, out: int) -> int:
@@ -682,13 +669,11 @@ def act_workspace_bytes(n: int, m: int, T: int, dim: int, out: int) -> int:
 def act_grad(packed, dY, mask, G, offset: int, dim: int, workspace=None, stream=None):
     """Gradient of W [dim, out] of Y = A W from packed A and dY [n, m, T, out] (bfloat16 rows), at
     ``offset`` of the rows of G [n, m, ld]."""
-    torch = _torch or _use_torch()
-    n, m, T, out = dY.shape
-    d, ldy, dtype = _rows(dY, "dY", (n, m, T))
+    n, m, T, out = shape = dY.shape
+    d, ldy, dtype = _rows(dY, "dY", shape)
     if dtype != BF16:
         raise TypeError("dY must be bfloat16")
     g, ld = _params(G, "G", (n, m), offset, dim * out)
     ws, ws_bytes = _workspace(workspace)
-    with _On(G, dY, packed, workspace):
-        _check(load().nbsgd_act_grad(_packed(packed, n, m, T, dim), d, ldy, n, m, T, dim, out,
-                                      _u8(mask, (n, m)), g, ld, ws, ws_bytes, _stream(G, stream)))
+    _call(load().nbsgd_act_grad, stream, G, (dY, packed, workspace),
+          (_packed(packed, n, m, T, dim), d, ldy, n, m, T, dim, out, _u8(mask, (n, m)), g, ld, ws, ws_bytes))
