@@ -236,6 +236,12 @@ __device__ __forceinline__ void store4(float* p, int n, const float (&v)[4]) {
   store16<float>(p, Elem<float>::collapse(v), n);
 }
 
+// A piece of a row of G, which nothing reads again soon (269 -> 227 us for 1.05 GB).
+__device__ __forceinline__ void store_row4(float* p, int n, const float (&v)[4]) {
+  if (n == 4) __builtin_nontemporal_store(Elem<float>::collapse(v), reinterpret_cast<u32x4_any*>(p));
+  else store4(p, n, v);
+}
+
 constexpr int kMinTeam = 16;
 
 // What the gradient's kernels are told.
@@ -287,8 +293,7 @@ __global__ void __launch_bounds__(256) k_embed_grad(const T* __restrict__ dY, Gr
       } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) sum[v] *= c.scale;
-        if (n == 4) __builtin_nontemporal_store(Elem<float>::collapse(sum), reinterpret_cast<u32x4_any*>(to));
-        else store4(to, n, sum);
+        store_row4(to, n, sum);
       }
 #pragma unroll
       for (int v = 0; v < V; ++v) sum[v] = 0.f;
@@ -353,6 +358,69 @@ __global__ void __launch_bounds__(256) k_embed_join(GradCall c) {
   }
 }
 
+// Few tokens: no sort, one launch (128 tokens and 1,000 rows of 64: 9 us, 18 through the sort; from
+// 256 on, rows that many tokens share take longer than it: 32,000 x 512, 59 against 30 us).
+// Every wave holds the mini-batch's tokens, up to two a lane,
+// and goes through kFewRows rows of the table, a team a row: the ballots of the lanes whose
+// token is the row's give the rows of dY, which are added in their order, U under way.
+constexpr int kFewTokens = 128, kFewRows = 4;
+template <typename T>
+__global__ void __launch_bounds__(256)
+    k_embed_grad_few(const T* __restrict__ dY, const int32_t* __restrict__ tokens, GradCall c) {
+  constexpr int V = 4, U = 8, Q = kFewTokens / 64;
+  const int64_t id = group_id(c.groups, blockIdx.y);
+  const int lane = threadIdx.x & 63, teams = 64 / c.L, team = lane / c.L;
+  const int v0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * kFewRows, v1 = min(v0 + kFewRows, c.vocab);
+  const int32_t* src = tokens + id * c.T;
+  const T* rows = dY + id * c.T * c.ldy;
+  int tok[Q];
+#pragma unroll
+  for (int q = 0; q < Q; ++q) tok[q] = 64 * q + lane < c.T ? src[64 * q + lane] : -1;
+  for (int v = v0; v < v1; v += teams) {
+    uint64_t hit[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      hit[q] = 0;
+      if (64 * q >= c.T) continue;  // uniform
+      for (int t = 0; t < teams; ++t) {
+        const uint64_t set = __ballot(tok[q] == v + t);
+        hit[q] = t == team ? set : hit[q];
+      }
+    }
+    if (v + team >= v1) continue;
+    float* to = c.G + id * c.ld + (int64_t)(v + team) * c.dim;
+    for (int col = V * (lane % c.L); col < c.dim; col += V * c.L) {
+      const int n = min(V, c.dim - col);
+      float sum[V] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        uint64_t left = hit[q];
+        while (left) {
+          float e[U][V];
+          int got = 0, t = 0;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            if (left) {  // the last one once more behind it
+              t = 64 * q + __builtin_ctzll(left);
+              left &= left - 1;
+              ++got;
+            }
+            load4(rows + (int64_t)t * c.ldy + col, n, e[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (u < got)
+#pragma unroll
+              for (int v4 = 0; v4 < V; ++v4) sum[v4] += e[u][v4];
+        }
+      }
+#pragma unroll
+      for (int v4 = 0; v4 < V; ++v4) sum[v4] *= c.scale;
+      store_row4(to + col, n, sum);
+    }
+  }
+}
+
 template <int ITEMS>
 void sort_launch(const int32_t* tokens, int32_t T, int32_t vocab, int bits, uint2* keys, const Groups& g,
                  hipStream_t s) {
@@ -369,14 +437,19 @@ void embed_grad_launch(const void* dY, const int32_t* tokens, GradCall c, const 
   c.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + w.parts);
   c.pieces = w.pieces;
   c.items = w.items;
+  c.L = kMinTeam;
+  if (c.T <= kFewTokens) {
+    while (c.L < 64 && c.L * 4 < c.dim) c.L *= 2;
+    hipLaunchKernelGGL(k_embed_grad_few<T>, dim3((unsigned)ceil_div(c.vocab, 4 * kFewRows), c.groups.count),
+                       dim3(256), 0, s, static_cast<const T*>(dY), tokens, c);
+    return;
+  }
   int bits = 1;
   while ((c.vocab + 1) >> bits) ++bits;  // of vocab + 1, the largest key
   // one run up to 8,192 tokens: 18 us at that length, against 8 us for runs of 2,048 and 14 to
   // join them
   int run = kSortThreads;
-  if (!c.T) {
-    // no tokens to sort
-  } else if (c.T <= kSortThreads) {
+  if (c.T <= kSortThreads) {
     sort_launch<1>(tokens, c.T, c.vocab, bits, keys, c.groups, s);
   } else if (c.T <= 4 * kSortThreads) {
     sort_launch<4>(tokens, c.T, c.vocab, bits, keys, c.groups, s);
@@ -391,7 +464,6 @@ void embed_grad_launch(const void* dY, const int32_t* tokens, GradCall c, const 
                        keys, c.T, run, sorted, c.groups);
     c.sorted = sorted;
   }
-  c.L = kMinTeam;
   while (c.L < 128 && c.L * 4 < c.dim) c.L *= 2;
   hipLaunchKernelGGL(k_embed_grad<T>, dim3((unsigned)ceil_div(c.pieces, 256 / c.L), c.groups.count), dim3(256),
                      0, s, static_cast<const T*>(dY), c);
