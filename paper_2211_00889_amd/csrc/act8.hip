@@ -334,39 +334,51 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) acc[a][j][k] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
+  // The operands of a step: A[h] made while the MFMAs of the step before run, B's fragments read
+  // RING ahead of their use.  The scheduler is told the mix, which it otherwise undoes.
+  constexpr int F = 4 * JT, RING = F < 4 ? F : 4;
+  bf16x8 A[2][MT];
+  auto make_a = [&](int h, int st) {
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+      A[h][a] = unpack8(qa[h][a],
+                        __builtin_bit_cast(float, (sa[a] >> (16 * (st & 1) + 8 * h) & 0xffu) << 23));
+  };
+  auto read_b = [&](int buf, int h, int f) {
+    return __builtin_bit_cast(bf16x8, Bs[buf][4 * h + g][f % 4 * Q + 16 * (JT * wn + f / 4) + i]);
+  };
   if (stages > 0) {
     load(0);
     stage(0);
+    make_a(0, 0);
   }
   __syncthreads();
   for (int st = 0; st < stages; ++st) {
     const int buf = st & 1;
-    u32x2 q[2][MT];
-    uint32_t sb[MT];
-#pragma unroll
-    for (int a = 0; a < MT; ++a) {
-      q[0][a] = qa[0][a], q[1][a] = qa[1][a];
-      sb[a] = sa[a] >> (16 * (st & 1));
-    }
+    make_a(1, st);
     if (st + 1 < stages) load(st + 1);
+    bf16x8 B[RING];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      bf16x8 A[MT];
+    for (int f = 0; f < RING; ++f) B[f] = read_b(buf, 0, f);
+#pragma unroll
+    for (int f = 0; f < 2 * F; ++f) {
+      const int h = f / F;
 #pragma unroll
       for (int a = 0; a < MT; ++a)
-        A[a] = unpack8(q[h][a], __builtin_bit_cast(float, (sb[a] >> (8 * h) & 0xffu) << 23));
-#pragma unroll
-      for (int j = 0; j < JT; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const bf16x8 B = __builtin_bit_cast(bf16x8, Bs[buf][4 * h + g][k * Q + 16 * (JT * wn + j) + i]);
-#pragma unroll
-          for (int a = 0; a < MT; ++a)
-            acc[a][j][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[a], B, acc[a][j][k], 0, 0, 0);
-        }
+        acc[a][f % F / 4][f % 4] =
+            __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[h][a], B[f % RING], acc[a][f % F / 4][f % 4], 0, 0, 0);
+      if (f + RING < 2 * F) B[f % RING] = read_b(buf, (f + RING) / F, (f + RING) % F);
     }
+    __builtin_amdgcn_sched_group_barrier(0x100, RING, 0);
+#pragma unroll
+    for (int f = 0; f < 2 * F - RING; ++f) {
+      __builtin_amdgcn_sched_group_barrier(0x008, MT, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, MT * RING, 0);
     if (st + 1 < stages) {
       stage(buf ^ 1);
+      make_a(0, st + 1);
       __syncthreads();
     }
   }

@@ -360,9 +360,9 @@ __global__ void __launch_bounds__(256) k_embed_join(GradCall c) {
 
 // Few tokens: no sort, one launch (128 tokens and 1,000 rows of 64: 9 us, 18 through the sort; from
 // 256 on, rows that many tokens share take longer than it: 32,000 x 512, 59 against 30 us).
-// Every wave holds the mini-batch's tokens, up to two a lane,
-// and goes through kFewRows rows of the table, a team a row: the ballots of the lanes whose
-// token is the row's give the rows of dY, which are added in their order, U under way.
+// Every wave holds the mini-batch's tokens, up to two a lane, and goes through kFewRows rows of
+// the table, a team a row: the ballots of the lanes whose token is the row's give the rows of
+// dY, which are added in their order, U under way.
 constexpr int kFewTokens = 128, kFewRows = 4;
 template <typename T>
 __global__ void __launch_bounds__(256)
