@@ -200,10 +200,10 @@ __global__ void __launch_bounds__(256)
 //      four fragments are four consecutive columns.
 // A wave takes 16 MT channels x 64 JT columns, WM x WN waves a tile.  Two buffers of B, one
 // barrier a stage; the next stage's loads are under way during this one's products.
-template <int MT, int JT, int WM, int WN>
+template <int MT, int JT, int WM, int WN, int HB>
 struct GradTile {
   static constexpr int kThreads = 64 * WM * WN, BM = 16 * MT * WM, BN = 64 * JT * WN;
-  static constexpr int kTokens = 64, kOcts = kTokens / 8;
+  static constexpr int kTokens = kActBlock * HB, kOcts = kTokens / 8;
   static constexpr int kCells = kOcts * BN / 4 / kThreads;  // of 8 tokens x 4 columns, a thread
 };
 
@@ -238,9 +238,9 @@ __device__ __forceinline__ bf16x8 unpack8(u32x2 q, float step) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
-template <int MT, int JT, int WM, int WN>
+template <int MT, int JT, int WM, int WN, int HB>
 __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
-  using S = GradTile<MT, JT, WM, WN>;
+  using S = GradTile<MT, JT, WM, WN, HB>;
   constexpr int BN = S::BN, Q = BN / 4, NC = S::kCells;
   __shared__ __attribute__((aligned(16))) u32x4 Bs[2][S::kOcts][BN];
   // an XCD (workgroup b runs on XCD b % 8) takes a run of neighbouring tiles, which read the same
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
   const int k0 = tm * S::BM + 16 * MT * wm, c0 = tn * BN;
   const int blk0 = part * c.per, blk1 = min(blk0 + c.per, (int)c.lay.blocks);
-  const int stages = (blk1 - blk0 + 1) / 2;
+  const int stages = (blk1 - blk0 + HB - 1) / HB;
 
   const uint8_t* base = c.packed + id * c.lay.bytes;
   const __bf16* rows = c.dY + id * c.T * c.ldy + c0;
@@ -275,12 +275,12 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
   }
   const bool whole = c0 + BN <= c.cols;  // every column of the tile is there
 
-  u32x2 qa[2][MT], rb[NC][8];
+  u32x2 qa[HB][MT], rb[NC][8];
   uint32_t sa[MT];
   auto load = [&](int st) {
-    const int b = blk0 + 2 * st;
+    const int b = blk0 + HB * st;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < HB; ++h) {
       const uint8_t* p = base + (int64_t)min(b + h, blk1 - 1) * c.dim * kActBlock;
 #pragma unroll
       for (int a = 0; a < MT; ++a) qa[h][a] = *reinterpret_cast<const u32x2*>(p + aoff[a]);
@@ -337,12 +337,12 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
   // The operands of a step: A[h] made while the MFMAs of the step before run, B's fragments read
   // RING ahead of their use.  The scheduler is told the mix, which it otherwise undoes.
   constexpr int F = 4 * JT, RING = F < 4 ? F : 4;
-  bf16x8 A[2][MT];
+  bf16x8 A[HB][MT];
   auto make_a = [&](int h, int st) {
 #pragma unroll
     for (int a = 0; a < MT; ++a)
       A[h][a] = unpack8(qa[h][a],
-                        __builtin_bit_cast(float, (sa[a] >> (16 * (st & 1) + 8 * h) & 0xffu) << 23));
+                        __builtin_bit_cast(float, (sa[a] >> (8 * (HB * st % 4 + h)) & 0xffu) << 23));
   };
   auto read_b = [&](int buf, int h, int f) {
     return __builtin_bit_cast(bf16x8, Bs[buf][4 * h + g][f % 4 * Q + 16 * (JT * wn + f / 4) + i]);
@@ -355,23 +355,24 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
   __syncthreads();
   for (int st = 0; st < stages; ++st) {
     const int buf = st & 1;
-    make_a(1, st);
+#pragma unroll
+    for (int h = 1; h < HB; ++h) make_a(h, st);
     if (st + 1 < stages) load(st + 1);
     bf16x8 B[RING];
 #pragma unroll
     for (int f = 0; f < RING; ++f) B[f] = read_b(buf, 0, f);
 #pragma unroll
-    for (int f = 0; f < 2 * F; ++f) {
+    for (int f = 0; f < HB * F; ++f) {
       const int h = f / F;
 #pragma unroll
       for (int a = 0; a < MT; ++a)
         acc[a][f % F / 4][f % 4] =
             __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[h][a], B[f % RING], acc[a][f % F / 4][f % 4], 0, 0, 0);
-      if (f + RING < 2 * F) B[f % RING] = read_b(buf, (f + RING) / F, (f + RING) % F);
+      if (f + RING < HB * F) B[f % RING] = read_b(buf, (f + RING) / F, (f + RING) % F);
     }
     __builtin_amdgcn_sched_group_barrier(0x100, RING, 0);
 #pragma unroll
-    for (int f = 0; f < 2 * F - RING; ++f) {
+    for (int f = 0; f < HB * F - RING; ++f) {
       __builtin_amdgcn_sched_group_barrier(0x008, MT, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
@@ -418,13 +419,13 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-template <int MT, int JT, int WM, int WN>
+template <int MT, int JT, int WM, int WN, int HB>
 void grad_launch(GradCall c, hipStream_t s) {
-  using S = GradTile<MT, JT, WM, WN>;
+  using S = GradTile<MT, JT, WM, WN, HB>;
   c.tm = (int32_t)ceil_div(c.dim, S::BM);
   c.tn = (int32_t)ceil_div(c.cols, S::BN);
   c.items = c.tm * c.tn * c.parts * c.groups.count;
-  hipLaunchKernelGGL((k_act8_grad<MT, JT, WM, WN>), dim3(8 * (unsigned)ceil_div(c.items, 8)),
+  hipLaunchKernelGGL((k_act8_grad<MT, JT, WM, WN, HB>), dim3(8 * (unsigned)ceil_div(c.items, 8)),
                      dim3(S::kThreads), 0, s, c);
 }
 
@@ -546,9 +547,9 @@ extern "C" nbsgd_status nbsgd_act_grad(const void* packed, const void* dY, int64
   // The largest tile that leaves no CU without one: its products per byte of LDS and of L2 are
   // the most.
   const int64_t each = (int64_t)c.parts * g.count;
-  if (each * ceil_div(dim, 256) * ceil_div(out, 256) >= kTileEnough) grad_launch<2, 4, 8, 1>(c, s);
-  else if (each * ceil_div(dim, 128) * ceil_div(out, 128) >= kTileEnough) grad_launch<4, 1, 2, 2>(c, s);
-  else grad_launch<2, 1, 2, 2>(c, s);
+  if (each * ceil_div(dim, 256) * ceil_div(out, 256) >= kTileEnough) grad_launch<2, 4, 8, 1, 4>(c, s);
+  else if (each * ceil_div(dim, 128) * ceil_div(out, 128) >= kTileEnough) grad_launch<4, 1, 2, 2, 2>(c, s);
+  else grad_launch<2, 1, 2, 2, 2>(c, s);
   if (c.parts > 1)
     hipLaunchKernelGGL(k_act8_parts, dim3((unsigned)std::min<int64_t>(ceil_div(size, 256), 1024), g.count),
                        dim3(256), 0, s, ws, c.parts, size, G, ld, g);
