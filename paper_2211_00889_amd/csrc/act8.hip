@@ -358,6 +358,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
 #pragma unroll
     for (int h = 1; h < HB; ++h) make_a(h, st);
     if (st + 1 < stages) load(st + 1);
+    // the products first: the two waves of a SIMD would otherwise stage and multiply in step
+    __builtin_amdgcn_s_setprio(1);
     bf16x8 B[RING];
 #pragma unroll
     for (int f = 0; f < RING; ++f) B[f] = read_b(buf, 0, f);
@@ -377,6 +379,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
     __builtin_amdgcn_sched_group_barrier(0x008, MT * RING, 0);
+    __builtin_amdgcn_s_setprio(0);
     if (st + 1 < stages) {
       stage(buf ^ 1);
       make_a(0, st + 1);
