@@ -231,13 +231,12 @@ __device__ __forceinline__ void from_lds(const float* p, float (&v)[V]) {
 #pragma unroll
   for (int k = 0; k < V; ++k) v[k] = r[k];
 }
-// Forward.  PAIRS: only each tile's composition, to `pairs` (the first of the three kernels
-// that split a sequence over workgroups); otherwise the states, from `carry` (the state at the
-// start of every tile) where the sequence is split, else from h0.
-template <typename T, bool PAIRS, bool WHOLE>
+// Forward, from h0, or from `carry` (the state at the start of every tile) where the sequence is
+// split over workgroups.
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(64 * kScanWaves, 2)
     k_scan(Call c, const float* __restrict__ h0, const float* __restrict__ carry,
-           float* __restrict__ pairs, T* __restrict__ h, int64_t ldh, float* __restrict__ h_last,
+           T* __restrict__ h, int64_t ldh, float* __restrict__ h_last,
            float* __restrict__ states) {
   using L = Lanes<T>;
   constexpr int V = L::V, K = L::K, CH = L::CH;
@@ -263,7 +262,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
   load_bias<V>(c, w, w.col + o, bias);
   const int tile0 = w.chunk * c.chunk, tile1 = min(tile0 + c.chunk, c.tiles);
   float s = 0.f;
-  if (!PAIRS && own < c.dim) {
+  if (own < c.dim) {
     if (carry) s = carry[(w.seq * c.tiles + tile0) * c.dim + own];
     else if (h0) s = h0[w.seq * c.dim + own];
   }
@@ -284,18 +283,11 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     const int t = tile * kScanTile + at, buf = tile & 1;
     const bool full = (tile + 1) * kScanTile <= w.len;
     if (tile * kScanTile >= w.len) {  // uniform: nothing left of the sequence
-      if constexpr (PAIRS) {
-        if (keeper) {
-          const int64_t cell = (w.seq * c.tiles + tile) * c.dim + own;
-          *reinterpret_cast<f32x2*>(pairs + 2 * cell) = (f32x2){1.f, 0.f};
-        }
-      } else {
-        if (states && keeper) states[(w.seq * c.tiles + tile) * c.dim + own] = s;
-        T* to = out0 + (int64_t)(tile * kScanTile + 32 * wave) * ldh;
+      if (states && keeper) states[(w.seq * c.tiles + tile) * c.dim + own] = s;
+      T* to = out0 + (int64_t)(tile * kScanTile + 32 * wave) * ldh;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-          if (n > 0 && t + k < c.T) store_row<T, WHOLE>(row_at(to + k * ldh, ih), (u32x2){0u, 0u}, n);
-      }
+      for (int k = 0; k < K; ++k)
+        if (n > 0 && t + k < c.T) store_row<T, WHOLE>(row_at(to + k * ldh, ih), (u32x2){0u, 0u}, n);
       continue;
     }
     float a[K][V], b[K][V], A[V], B[V];
@@ -333,13 +325,6 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       TB = fmaf(qa, TB, qb);
       TA *= qa;
     }
-    if constexpr (PAIRS) {
-      if (keeper) {
-        const int64_t cell = (w.seq * c.tiles + tile) * c.dim + own;
-        *reinterpret_cast<f32x2*>(pairs + 2 * cell) = (f32x2){TA, TB};
-      }
-      continue;
-    }
     if (states && keeper) states[(w.seq * c.tiles + tile) * c.dim + own] = s;
     s = fmaf(TA, s, TB);
     start[wave][oc] = mine;
@@ -359,7 +344,70 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       if (n > 0 && (full || t + k < c.T)) store_row<T, WHOLE>(row_at(to + k * ldh, ih), r, n);
     }
   }
-  if (!PAIRS && h_last && tile1 == c.tiles && keeper) h_last[w.seq * c.dim + own] = s;
+  if (h_last && tile1 == c.tiles && keeper) h_last[w.seq * c.dim + own] = s;
+}
+
+// Composition of every tile of a split sequence, to `pairs`: of h -> a h + (1 - a) x (p is x), or,
+// REVERSE, of mu -> a (dh + mu) from a tile's last token to its first (p is dh).  As a rule a
+// tile a workgroup, and few enough registers for four of them a CU: what it waits for is its rows.
+template <typename T, bool REVERSE, bool WHOLE>
+__global__ void __launch_bounds__(64 * kScanWaves, 8)
+    k_scan_pairs(Call c, const T* __restrict__ p, int64_t ldp, float* __restrict__ pairs) {
+  using L = Lanes<T>;
+  constexpr int V = L::V, K = L::K, CH = L::CH;
+  __shared__ __attribute__((aligned(16))) float tot[2][kScanWaves][CH];
+  const Where w = locate<CH>(c, false);
+  if (w.seq < 0) return;  // uniform
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int o = lane % L::LV * V, sub = lane / L::LV;
+  const int n = c.dim - (w.col + o), own = w.col + (lane & (CH - 1));
+  const uint32_t col = n > 0 ? o : 0;
+  float bias[V];
+  load_bias<V>(c, w, w.col + o, bias);
+  for (int tile = w.chunk * c.chunk; tile < min((w.chunk + 1) * c.chunk, c.tiles); ++tile) {
+    const int64_t row = w.seq * c.T + tile * kScanTile + 32 * wave;
+    const bool full = (tile + 1) * kScanTile <= w.len;
+    const int live = w.len - tile * kScanTile - 32 * wave - sub * K;
+    u32x2 rp[K], rg[K];
+    load_run<T, WHOLE>(p + row * ldp + w.col, ldp, (uint32_t)(sub * K * (int)ldp + (int)col) * (uint32_t)sizeof(T),
+                       full, live, n, 0u, rp);
+    load_run<T, WHOLE>(static_cast<const T*>(c.g) + row * c.ldx + w.col, c.ldx,
+                       (uint32_t)(sub * K * (int)c.ldx + (int)col) * (uint32_t)sizeof(T), full, live, n,
+                       Word<T>::kPast, rg);
+    float A[V], B[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) A[v] = 1.f, B[v] = 0.f;
+#pragma unroll
+    for (int q = 0; q < K; ++q) {
+      const int k = REVERSE ? K - 1 - q : q;
+      float pv[V], gv[V];
+      expand(rp[k], pv);
+      expand(rg[k], gv);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const Gate u = gate<sizeof(T) == 4>(gv[v] + bias[v]);
+        B[v] = REVERSE ? u.a * (pv[v] + B[v]) : fmaf(u.a, B[v], u.rest * pv[v]);
+        A[v] *= u.a;
+      }
+    }
+    float EA[V], EB[V];
+    compose<T, !REVERSE>(sub, A, B, EA, EB);
+    if (sub == (REVERSE ? 0 : L::SUBS - 1)) {
+      to_lds<V>(&tot[0][wave][o], A);
+      to_lds<V>(&tot[1][wave][o], B);
+    }
+    __syncthreads();
+    if (wave == 0 && lane < CH && own < c.dim) {
+      float TA = 1.f, TB = 0.f;
+      for (int y = 0; y < kScanWaves; ++y) {
+        const int q = REVERSE ? kScanWaves - 1 - y : y;
+        TB = fmaf(tot[0][q][lane], TB, tot[1][q][lane]);
+        TA *= tot[0][q][lane];
+      }
+      *reinterpret_cast<f32x2*>(pairs + 2 * ((w.seq * c.tiles + tile) * c.dim + own)) = (f32x2){TA, TB};
+    }
+    __syncthreads();
+  }
 }
 
 // State (or gradient, REVERSE) at the start of every tile of a split sequence, from the tiles'
@@ -405,12 +453,12 @@ __global__ void __launch_bounds__(512)
   }
 }
 
-// Backward, tiles from the last to the first; PAIRS and carry as in k_scan, for mu.
-template <typename T, bool PAIRS, bool WHOLE>
+// Backward, tiles from the last to the first; carry as in k_scan, for mu.
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(64 * kScanWaves, 2)
     k_scan_grad(Call c, const float* __restrict__ states, const T* __restrict__ dh, int64_t lddh,
                 const float* __restrict__ dh_last, const float* __restrict__ carry,
-                float* __restrict__ pairs, T* __restrict__ dx, T* __restrict__ dg,
+                T* __restrict__ dx, T* __restrict__ dg,
                 float* __restrict__ dh0, float* __restrict__ part) {
   using L = Lanes<T>;
   constexpr int V = L::V, K = L::K, CH = L::CH;
@@ -435,7 +483,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
   load_bias<V>(c, w, w.col + o, bias);
   const int tile0 = w.chunk * c.chunk, tile1 = min(tile0 + c.chunk, c.tiles);
   float mu = 0.f;
-  if (!PAIRS && own < c.dim) {
+  if (own < c.dim) {
     if (carry) mu = carry[(w.seq * c.tiles + tile1 - 1) * c.dim + own];
     else if (dh_last) mu = dh_last[w.seq * c.dim + own];
   }
@@ -449,10 +497,8 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     const int t = tile * kScanTile;
     const int64_t row = (int64_t)(t + 32 * wave) * c.ldx;
     const bool full = t + kScanTile <= w.len;
-    if constexpr (!PAIRS) {
-      load_run<T, WHOLE>(x + row, c.ldx, ix, full, w.len - t - at, n, 0u, rx);
-      s = own < c.dim ? states[(w.seq * c.tiles + tile) * c.dim + own] : 0.f;
-    }
+    load_run<T, WHOLE>(x + row, c.ldx, ix, full, w.len - t - at, n, 0u, rx);
+    s = own < c.dim ? states[(w.seq * c.tiles + tile) * c.dim + own] : 0.f;
     load_run<T, WHOLE>(g + row, c.ldx, ix, full, w.len - t - at, n, Word<T>::kPast, rg);
     load_run<T, WHOLE>(d + (int64_t)(t + 32 * wave) * lddh, lddh, id, full, w.len - t - at, n, 0u, rd);
   };
@@ -464,23 +510,16 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     T *tg = dg0 + (int64_t)(tile * kScanTile + 32 * wave) * c.ldx;
     float* sums = part + ((w.seq * c.tiles + tile) * waves + wave) * c.dim + w.col + o;
     if (tile * kScanTile >= w.len) {  // uniform: behind the sequence
-      if constexpr (PAIRS) {
-        if (keeper) {
-          const int64_t cell = (w.seq * c.tiles + tile) * c.dim + own;
-          *reinterpret_cast<f32x2*>(pairs + 2 * cell) = (f32x2){1.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (n > 0 && t + k < c.T) {
+          store_row<T, WHOLE>(row_at(tx + k * c.ldx, ix), (u32x2){0u, 0u}, n);
+          store_row<T, WHOLE>(row_at(tg + k * c.ldx, ix), (u32x2){0u, 0u}, n);
         }
-      } else {
+      if (part && sub == 0)
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-          if (n > 0 && t + k < c.T) {
-            store_row<T, WHOLE>(row_at(tx + k * c.ldx, ix), (u32x2){0u, 0u}, n);
-            store_row<T, WHOLE>(row_at(tg + k * c.ldx, ix), (u32x2){0u, 0u}, n);
-          }
-        if (part && sub == 0)
-#pragma unroll
-          for (int v = 0; v < V; ++v)
-            if (v < n) sums[v] = 0.f;
-      }
+        for (int v = 0; v < V; ++v)
+          if (v < n) sums[v] = 0.f;
       if (tile > tile0) load_tile(tile - 1);
       continue;
     }
@@ -496,13 +535,13 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     for (int k = 0; k < K; ++k) {
       float gv[V], xv[V];
       expand(cg[k], gv);
-      if constexpr (!PAIRS) expand(cx[k], xv);
+      expand(cx[k], xv);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const Gate u = gate<sizeof(T) == 4>(gv[v] + bias[v]);
         a[k][v] = u.a;
         rest[k][v] = u.rest;
-        if constexpr (!PAIRS) B[v] = fmaf(u.a, B[v], u.rest * xv[v]);
+        B[v] = fmaf(u.a, B[v], u.rest * xv[v]);
         A[v] *= u.a;
       }
     }
@@ -521,12 +560,10 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       to_lds<V>(&tot[buf][0][wave][o], RA);
       to_lds<V>(&tot[buf][1][wave][o], R);
     }
-    if constexpr (!PAIRS) {
-      compose<T, true>(sub, A, B, EA, EB);
-      if (sub == L::SUBS - 1) {
-        to_lds<V>(&tot[buf][2][wave][o], A);
-        to_lds<V>(&tot[buf][3][wave][o], B);
-      }
+    compose<T, true>(sub, A, B, EA, EB);
+    if (sub == L::SUBS - 1) {
+      to_lds<V>(&tot[buf][2][wave][o], A);
+      to_lds<V>(&tot[buf][3][wave][o], B);
     }
     __syncthreads();
     float TA = 1.f, TR = 0.f, mine = 0.f;
@@ -535,13 +572,6 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       const float qa = tot[buf][0][y][oc], qr = tot[buf][1][y][oc];
       TR = fmaf(qa, TR, qr);
       TA *= qa;
-    }
-    if constexpr (PAIRS) {
-      if (keeper) {
-        const int64_t cell = (w.seq * c.tiles + tile) * c.dim + own;
-        *reinterpret_cast<f32x2*>(pairs + 2 * cell) = (f32x2){TA, TR};
-      }
-      continue;
     }
     float PA = 1.f, PB = 0.f;
     for (int y = 0; y < wave; ++y) {
@@ -607,7 +637,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       }
     }
   }
-  if (!PAIRS && dh0 && tile0 == 0 && keeper) dh0[w.seq * c.dim + own] = mu;
+  if (dh0 && tile0 == 0 && keeper) dh0[w.seq * c.dim + own] = mu;
 }
 
 // Sequences of at most kShort tokens (a served step above all), a channel a thread: the tile
@@ -736,6 +766,13 @@ nbsgd_status check_operand(const char* name, const void* p, int64_t rows, int64_
   return check_rows(name, p, rows, dim, ld, e);
 }
 
+// Grid of the compositions of a split call: a workgroup a tile, up to the limits of a grid.
+dim3 tile_grid(Call* c, const Deal& d) {
+  c->chunk = (int32_t)ceil_div(d.cols * d.seqs * c->tiles, 1 << 20);
+  c->items = (int32_t)(d.cols * d.seqs * ceil_div(c->tiles, c->chunk));
+  return dim3(8 * (unsigned)ceil_div(c->items, 8));
+}
+
 nbsgd_status fill_call(Call* c, const void* x, const void* g, int64_t ldx, int32_t n, int32_t m,
                        int32_t batch, int32_t Tn, int32_t dim, const float* bias, int64_t ld,
                        const int32_t* lengths, const uint8_t* mask) {
@@ -773,12 +810,13 @@ nbsgd_status scan_forward(Call& c, const ScanSpace& w, const float* h0, void* h,
   if (d.chunks > 1) {
     float* pairs = reinterpret_cast<float*>(static_cast<char*>(ws) + w.pairs);
     carry = reinterpret_cast<float*>(static_cast<char*>(ws) + w.carry);
-    hipLaunchKernelGGL((k_scan<T, true, WHOLE>), grid, block, 0, s, c, h0, nullptr, pairs, out, ldh, nullptr,
-                       nullptr);
+    Call each = c;
+    hipLaunchKernelGGL((k_scan_pairs<T, false, WHOLE>), tile_grid(&each, d), block, 0, s, each,
+                       static_cast<const T*>(c.x), c.ldx, pairs);
     hipLaunchKernelGGL(k_scan_carry<false>, dim3((unsigned)(ceil_div(c.dim, 64) * d.seqs)), dim3(512), 0, s, c, pairs,
                        h0, carry);
   }
-  hipLaunchKernelGGL((k_scan<T, false, WHOLE>), grid, block, 0, s, c, h0, carry, nullptr, out, ldh, h_last,
+  hipLaunchKernelGGL((k_scan<T, WHOLE>), grid, block, 0, s, c, h0, carry, out, ldh, h_last,
                      states);
   return launched("nbsgd_scan");
 }
@@ -807,13 +845,13 @@ nbsgd_status scan_backward(Call& c, const ScanSpace& w, const float* states, con
     if (d.chunks > 1) {
       float* pairs = reinterpret_cast<float*>(static_cast<char*>(ws) + w.pairs);
       carry = reinterpret_cast<float*>(static_cast<char*>(ws) + w.carry);
-      hipLaunchKernelGGL((k_scan_grad<T, true, WHOLE>), grid, block, 0, s, c, states, d_in, lddh, dh_last,
-                         nullptr, pairs, ox, og, nullptr, nullptr);
+      Call each = c;
+      hipLaunchKernelGGL((k_scan_pairs<T, true, WHOLE>), tile_grid(&each, d), block, 0, s, each, d_in, lddh,
+                         pairs);
       hipLaunchKernelGGL(k_scan_carry<true>, dim3((unsigned)(ceil_div(c.dim, 64) * d.seqs)), dim3(512), 0, s, c, pairs,
                          dh_last, carry);
     }
-    hipLaunchKernelGGL((k_scan_grad<T, false, WHOLE>), grid, block, 0, s, c, states, d_in, lddh, dh_last, carry,
-                       nullptr, ox, og, dh0, part);
+    hipLaunchKernelGGL((k_scan_grad<T, WHOLE>), grid, block, 0, s, c, states, d_in, lddh, dh_last, carry, ox, og, dh0, part);
   }
   if (Gbias)
     hipLaunchKernelGGL(k_scan_bias, dim3((unsigned)ceil_div(c.dim, 64), c.groups.count), dim3(1024), 0,
