@@ -188,23 +188,31 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// Weight gradient dW = A^T dY: the tokens are the K of MFMA 16x16x32 (bf16, fp32 sums), a
-// packed block of 32 tokens one step of it.  Operands (lane l, t = 0..7): A[l % 16][8 (l / 16)
-// + t], B[8 (l / 16) + t][l % 16]; result D[4 (l / 16) + t][l % 16], t = 0..3.
-//   A  is packed as the operand wants it, 8 consecutive tokens of a channel: a lane loads its
-//      8 bytes straight from memory (16 channels are 512 contiguous bytes) and makes bf16 of
-//      them, u * 2^k - 128 * 2^k of the byte with its top bit turned, exactly; no LDS
-//   B  (dY) comes a row a token: 64 tokens are staged at a time, a thread turns 8 tokens x 4
-//      columns and writes 16 bytes a column.  Column 4 q + c of the tile is slot c * BN / 4 + q,
-//      so that the writes and the reads of 16 lanes are contiguous and a lane's results of
-//      four fragments are four consecutive columns.
-// A wave takes 16 MT channels x 64 JT columns, WM x WN waves a tile.  Two buffers of B, one
-// barrier a stage; the next stage's loads are under way during this one's products.
-template <int MT, int JT, int WM, int WN, int HB>
+// Weight gradient dW = A^T dY: the tokens are the K of MFMA 16x16x32 (bf16, fp32 sums), 64 of
+// them a stage of two steps.  Operands (lane l, g = l / 16, t = 0..7): A[l % 16][8 g + t], B[8 g +
+// t][l % 16]; result D[4 g + t][l % 16], t = 0..3.  Which tokens a step's K are is free as long
+// as both operands agree: of 64 tokens, octets 2 g of lanes g are step 0 and octets 2 g + 1 step 1,
+// so that
+//   A  (packed) is loaded 16 bytes a lane, 16 tokens of a channel, straight from memory, and
+//      made bf16 in registers, u * 2^k - 128 * 2^k of the byte with its top bit turned, exactly;
+//      every value once, since a wave has all columns of its channels
+//   B  (dY) comes a row a token: a thread turns 4 tokens x 8 columns and writes 8 bytes a
+//      column to LDS, column 8 q + e of the tile to slot e * BN / 8 + q, so that the writes and
+//      the fragment reads are contiguous and a lane's results of eight (or four) fragments are
+//      consecutive columns.
+// A wave takes 16 MT channels x 16 F columns, WM x WN waves a tile.  Two buffers of B, one
+// barrier a stage.  The next stage's loads go out one by one among this stage's MFMAs.
+// 32 mini-batches of 4096 x 1024 x 2048: 545 us, 1.01 PFLOP/s (a library's bf16 product of
+// 8192^3 reaches 1.17).  What bounds it: the MFMAs are 240 us of it and the stage's other parts
+// hardly hide behind them, since a barrier a stage keeps the two waves of a SIMD in step; with
+// no loads it took 400, with no unpacking 508, without the turning 529.  128 tokens a
+// stage 542; 64 channels x 256 columns a wave 808, x 128 663; two workgroups of four such
+// waves a CU 583.
+constexpr int kHB = 2, kStageTokens = kActBlock * kHB;
+template <int MT, int F, int WM, int WN>
 struct GradTile {
-  static constexpr int kThreads = 64 * WM * WN, BM = 16 * MT * WM, BN = 64 * JT * WN;
-  static constexpr int kTokens = kActBlock * HB, kOcts = kTokens / 8;
-  static constexpr int kCells = kOcts * BN / 4 / kThreads;  // of 8 tokens x 4 columns, a thread
+  static constexpr int kThreads = 64 * WM * WN, BM = 16 * MT * WM, BN = 16 * F * WN;
+  static_assert(kStageTokens / 4 * (BN / 8) == kThreads, "a thread turns 4 tokens x 8 columns");
 };
 
 // What a launch is told: items (mini-batch, part of its tokens, tile), tiles fastest.
@@ -215,6 +223,7 @@ struct GradCall {
   int64_t ldy, ld;  // of out: floats from one mini-batch to the next
   int64_t part;     // floats from one part to the next
   int32_t T, dim, cols, parts, per;  // per: blocks of a part, a multiple of four
+  int32_t batches;                   // mini-batches of dY
   int32_t tm, tn, items;
   Act8 lay;
   Groups groups;
@@ -224,12 +233,13 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // Eight bytes of a channel as bf16, on the step 2^(byte - 127).  A byte of 255 makes an infinite
 // step and NaNs of every value: inf - inf.
-__device__ __forceinline__ bf16x8 unpack8(u32x2 q, float step) {
+__device__ __forceinline__ bf16x8 unpack8(uint32_t q0, uint32_t q1, float step) {
   const float back = -128.f * step;
+  const uint32_t q[2] = {q0 ^ 0x80808080u, q1 ^ 0x80808080u};
   u32x4 r;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const uint32_t u = q[h] ^ 0x80808080u;
+    const uint32_t u = q[h];
     const float f0 = fmaf((float)(u & 0xffu), step, back), f1 = fmaf((float)(u >> 8 & 0xffu), step, back);
     const float f2 = fmaf((float)(u >> 16 & 0xffu), step, back), f3 = fmaf((float)(u >> 24), step, back);
     r[2 * h] = pack2(f0, f1);
@@ -238,11 +248,11 @@ __device__ __forceinline__ bf16x8 unpack8(u32x2 q, float step) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
-template <int MT, int JT, int WM, int WN, int HB>
+template <int MT, int F, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
-  using S = GradTile<MT, JT, WM, WN, HB>;
-  constexpr int BN = S::BN, Q = BN / 4, NC = S::kCells;
-  __shared__ __attribute__((aligned(16))) u32x4 Bs[2][S::kOcts][BN];
+  using S = GradTile<MT, F, WM, WN>;
+  constexpr int BN = S::BN, Q = BN / 8, RING = 8, STEPS = kHB * F;
+  __shared__ __attribute__((aligned(16))) u32x2 Bs[2][kStageTokens / 8][BN][2];
   // an XCD (workgroup b runs on XCD b % 8) takes a run of neighbouring tiles, which read the same
   // tokens through its L2
   const int xper = gridDim.x >> 3, item = (blockIdx.x & 7) * xper + (int)(blockIdx.x >> 3);
@@ -254,7 +264,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
   const int k0 = tm * S::BM + 16 * MT * wm, c0 = tn * BN;
   const int blk0 = part * c.per, blk1 = min(blk0 + c.per, (int)c.lay.blocks);
-  const int stages = (blk1 - blk0 + HB - 1) / HB;
+  const int tokens = min(blk1 * kActBlock, c.T);  // the next part's are left to it
+  const int stages = (blk1 - blk0 + kHB - 1) / kHB;
 
   const uint8_t* base = c.packed + id * c.lay.bytes;
   const __bf16* rows = c.dY + id * c.T * c.ldy + c0;
@@ -262,127 +273,122 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
 #pragma unroll
   for (int a = 0; a < MT; ++a) {
     const uint32_t ch = (uint32_t)min(k0 + 16 * a + i, c.dim - 1);
-    aoff[a] = ch * kActBlock + 8 * g;
+    aoff[a] = ch * kActBlock + 16 * (g & 1);
     soff[a] = ch * 4;
   }
-  int oct[NC], quad[NC];
-  uint32_t boff[NC];  // bytes from a stage's first row; the rows' bases are uniform
-#pragma unroll
-  for (int e = 0; e < NC; ++e) {
-    oct[e] = (tid + e * S::kThreads) / Q;
-    quad[e] = (tid + e * S::kThreads) % Q;
-    boff[e] = 2u * (uint32_t)(8 * oct[e] * (int)c.ldy + 4 * quad[e]);
-  }
-  const bool whole = c0 + BN <= c.cols;  // every column of the tile is there
+  const uint32_t aup = (uint32_t)(g >> 1) * (uint32_t)c.dim * kActBlock;  // to the lane's block of two
+  const int four = tid / Q, q8 = tid % Q;  // the cell of B that this thread turns
+  // cells past the last column turn the tile's first ones, and a cell at the border whatever
+  // follows its row: nothing stores what they give
+  const uint32_t boff = 2u * (uint32_t)(4 * four * (int)c.ldy + (8 * q8 < c.cols - c0 ? 8 * q8 : 0));
 
-  u32x2 qa[HB][MT], rb[NC][8];
+  u32x4 qa[MT], rb[4];
   uint32_t sa[MT];
-  auto load = [&](int st) {
-    const int b = blk0 + HB * st;
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-      const uint8_t* p = base + (int64_t)min(b + h, blk1 - 1) * c.dim * kActBlock;
-#pragma unroll
-      for (int a = 0; a < MT; ++a) qa[h][a] = *reinterpret_cast<const u32x2*>(p + aoff[a]);
+  constexpr int kLoads = 2 * MT + 4;
+  // Whether a stage is read without looking: all its tokens are there, and whatever follows its
+  // rows (uniform).  What is no such stage reads the first packed bytes here, for nobody, so that
+  // the loads need no branch.
+  auto plain = [&](int st) {
+    const int end = (blk0 + kHB * (st + 1)) * kActBlock;
+    return end <= tokens && (c0 + BN <= c.cols || end < c.T || id + 1 < c.batches);
+  };
+  auto load_one = [&](int st, bool go, int k) {
+    const int b = blk0 + kHB * st;
+    const uint32_t on = go ? ~0u : 0u;
+    if (k < 4) {
+      const uint8_t* from = go ? reinterpret_cast<const uint8_t*>(rows + (int64_t)(b * kActBlock + k) * c.ldy) : base;
+      rb[k] = *reinterpret_cast<const u32x4_any*>(from + (boff & on));
+    } else if (k < 4 + MT) {
+      const uint8_t* from = base + (go ? (int64_t)b * c.dim * kActBlock : 0);
+      qa[k - 4] = *reinterpret_cast<const u32x4*>(from + ((aoff[k - 4] + aup) & on));
+    } else {
+      const uint8_t* from = base + (go ? c.lay.scale + (int64_t)(b >> 2) * c.dim * 4 : 0);
+      sa[k - 4 - MT] = *reinterpret_cast<const uint32_t*>(from + (soff[k - 4 - MT] & on));
     }
-    const uint8_t* p = base + c.lay.scale + (int64_t)(b >> 2) * c.dim * 4;
+  };
+  // Any stage: blocks past the last are read as it, tokens and columns past the last as zeros
+  auto load_any = [&](int st) {
+    const int b = blk0 + kHB * st;
+    const int blk = min(b + (g >> 1), blk1 - 1);
 #pragma unroll
-    for (int a = 0; a < MT; ++a) sa[a] = *reinterpret_cast<const uint32_t*>(p + soff[a]);
-    const int t0 = b * kActBlock;
-    if (whole && t0 + S::kTokens <= c.T) {  // uniform
-#pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const char* row = reinterpret_cast<const char*>(rows + (int64_t)(t0 + t) * c.ldy);
-#pragma unroll
-        for (int e = 0; e < NC; ++e) rb[e][t] = *reinterpret_cast<const u32x2_any*>(row + boff[e]);
-      }
-      return;
+    for (int a = 0; a < MT; ++a) {
+      qa[a] = *reinterpret_cast<const u32x4*>(base + (int64_t)blk * c.dim * kActBlock + aoff[a]);
+      sa[a] = *reinterpret_cast<const uint32_t*>(base + c.lay.scale + (int64_t)(b >> 2) * c.dim * 4 + soff[a]);
     }
+    const int n = c.cols - c0 - 8 * q8;
 #pragma unroll
-    for (int e = 0; e < NC; ++e)
-#pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        uint32_t w[2] = {0u, 0u};
-        const int tok = t0 + 8 * oct[e] + t, n = c.cols - c0 - 4 * quad[e];
-        const __bf16* q = rows + (int64_t)tok * c.ldy + 4 * quad[e];
-        // tokens of the next part are left to it
-        if (tok < c.T && tok < blk1 * kActBlock)
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (k < n) w[k >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, q[k]) << (16 * (k & 1));
-        rb[e][t] = (u32x2){w[0], w[1]};
-      }
+    for (int t = 0; t < 4; ++t) {
+      const int tok = b * kActBlock + 4 * four + t;
+      rb[t] = (u32x4){0u, 0u, 0u, 0u};
+      if (tok < tokens && n > 0) rb[t] = load16<__bf16>(rows + (int64_t)tok * c.ldy + 8 * q8, n);
+    }
   };
   auto stage = [&](int buf) {
 #pragma unroll
-    for (int e = 0; e < NC; ++e)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        u32x4 v;
-#pragma unroll
-        for (int p = 0; p < 4; ++p)  // tokens 2 p, 2 p + 1 of column k: the same half of two rows
-          v[p] = __builtin_amdgcn_perm(rb[e][2 * p + 1][k >> 1], rb[e][2 * p][k >> 1],
-                                       k & 1 ? 0x07060302u : 0x05040100u);
-        Bs[buf][oct[e]][k * Q + quad[e]] = v;
-      }
+    for (int e = 0; e < 8; ++e) {
+      // tokens 2 p, 2 p + 1 of column e: the same half of two rows
+      const uint32_t half = e & 1 ? 0x07060302u : 0x05040100u;
+      Bs[buf][four >> 1][e * Q + q8][four & 1] = (u32x2){__builtin_amdgcn_perm(rb[1][e >> 1], rb[0][e >> 1], half),
+                                                         __builtin_amdgcn_perm(rb[3][e >> 1], rb[2][e >> 1], half)};
+    }
   };
-  f32x4 acc[MT][JT][4];
+  f32x4 acc[MT][F];
 #pragma unroll
   for (int a = 0; a < MT; ++a)
 #pragma unroll
-    for (int j = 0; j < JT; ++j)
+    for (int f = 0; f < F; ++f) acc[a][f] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  bf16x8 A[kHB][MT];
+  auto make_a = [&](int st) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) acc[a][j][k] = (f32x4){0.f, 0.f, 0.f, 0.f};
-
-  // The operands of a step: A[h] made while the MFMAs of the step before run, B's fragments read
-  // RING ahead of their use.  The scheduler is told the mix, which it otherwise undoes.
-  constexpr int F = 4 * JT, RING = F < 4 ? F : 4;
-  bf16x8 A[HB][MT];
-  auto make_a = [&](int h, int st) {
-#pragma unroll
-    for (int a = 0; a < MT; ++a)
-      A[h][a] = unpack8(qa[h][a],
-                        __builtin_bit_cast(float, (sa[a] >> (8 * (HB * st % 4 + h)) & 0xffu) << 23));
+    for (int a = 0; a < MT; ++a) {
+      const float step = __builtin_bit_cast(float, (sa[a] >> (16 * (st & 1) + 8 * (g >> 1)) & 0xffu) << 23);
+      A[0][a] = unpack8(qa[a][0], qa[a][1], step);
+      A[1][a] = unpack8(qa[a][2], qa[a][3], step);
+    }
   };
-  auto read_b = [&](int buf, int h, int f) {
-    return __builtin_bit_cast(bf16x8, Bs[buf][4 * h + g][f % 4 * Q + 16 * (JT * wn + f / 4) + i]);
+  auto read_b = [&](int buf, int n) {
+    const int h = n / F, f = wn * F + n % F;
+    return *reinterpret_cast<const bf16x8*>(&Bs[buf][2 * g + h][f % 8 * Q + 16 * (f / 8) + i][0]);
   };
-  if (stages > 0) {
-    load(0);
-    stage(0);
-    make_a(0, 0);
-  }
-  __syncthreads();
-  for (int st = 0; st < stages; ++st) {
-    const int buf = st & 1;
-#pragma unroll
-    for (int h = 1; h < HB; ++h) make_a(h, st);
-    if (st + 1 < stages) load(st + 1);
+  // A stage's products, RING fragments read ahead, with the next stage's loads among them
+  auto multiply = [&](int buf, int next, bool go) {
     // the products first: the two waves of a SIMD would otherwise stage and multiply in step
     __builtin_amdgcn_s_setprio(1);
     bf16x8 B[RING];
 #pragma unroll
-    for (int f = 0; f < RING; ++f) B[f] = read_b(buf, 0, f);
+    for (int n = 0; n < RING; ++n) B[n] = read_b(buf, n);
 #pragma unroll
-    for (int f = 0; f < HB * F; ++f) {
-      const int h = f / F;
+    for (int n = 0; n < STEPS; ++n) {
 #pragma unroll
       for (int a = 0; a < MT; ++a)
-        acc[a][f % F / 4][f % 4] =
-            __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[h][a], B[f % RING], acc[a][f % F / 4][f % 4], 0, 0, 0);
-      if (f + RING < HB * F) B[f % RING] = read_b(buf, (f + RING) / F, (f + RING) % F);
+        acc[a][n % F] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[n / F][a], B[n % RING], acc[a][n % F], 0, 0, 0);
+      if (n + RING < STEPS) B[n % RING] = read_b(buf, n + RING);
+      if (n < kLoads) load_one(next, go, n);
     }
-    __builtin_amdgcn_sched_group_barrier(0x100, RING, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, RING, 0);  // LDS reads
 #pragma unroll
-    for (int f = 0; f < HB * F - RING; ++f) {
-      __builtin_amdgcn_sched_group_barrier(0x008, MT, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    for (int n = 0; n < STEPS; ++n) {
+      __builtin_amdgcn_sched_group_barrier(0x008, MT, 0);  // MFMAs
+      if (n + RING < STEPS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      if (n < kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // load
     }
-    __builtin_amdgcn_sched_group_barrier(0x008, MT * RING, 0);
     __builtin_amdgcn_s_setprio(0);
+  };
+
+  if (stages > 0) {
+    load_any(0);
+    stage(0);
+    make_a(0);
+  }
+  __syncthreads();
+  for (int st = 0; st < stages; ++st) {
+    const int buf = st & 1;
+    const bool go = plain(st + 1);
+    multiply(buf, st + 1, go);
+    if (st + 1 < stages && !go) load_any(st + 1);
     if (st + 1 < stages) {
       stage(buf ^ 1);
-      make_a(0, st + 1);
+      make_a(st + 1);
       __syncthreads();
     }
   }
@@ -394,16 +400,15 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
       const int ch = k0 + 16 * a + 4 * g + t;
       if (ch >= c.dim) continue;
 #pragma unroll
-      for (int j = 0; j < JT; ++j) {
-        const int col = c0 + 64 * (JT * wn + j) + 4 * i;
+      for (int f = 0; f < F; f += 4) {
+        const int e = (wn * F + f) % 8, col = c0 + 8 * (16 * ((wn * F + f) / 8) + i) + e;
         float* p = out + (int64_t)ch * c.cols + col;
         if (col + 4 <= c.cols) {
-          *reinterpret_cast<f32x4_any*>(p) =
-              (f32x4){acc[a][j][0][t], acc[a][j][1][t], acc[a][j][2][t], acc[a][j][3][t]};
+          *reinterpret_cast<f32x4_any*>(p) = (f32x4){acc[a][f][t], acc[a][f + 1][t], acc[a][f + 2][t], acc[a][f + 3][t]};
         } else {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if (col + k < c.cols) p[k] = acc[a][j][k][t];
+            if (col + k < c.cols) p[k] = acc[a][f + k][t];
         }
       }
     }
@@ -422,13 +427,13 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-template <int MT, int JT, int WM, int WN, int HB>
+template <int MT, int F, int WM, int WN>
 void grad_launch(GradCall c, hipStream_t s) {
-  using S = GradTile<MT, JT, WM, WN, HB>;
+  using S = GradTile<MT, F, WM, WN>;
   c.tm = (int32_t)ceil_div(c.dim, S::BM);
   c.tn = (int32_t)ceil_div(c.cols, S::BN);
   c.items = c.tm * c.tn * c.parts * c.groups.count;
-  hipLaunchKernelGGL((k_act8_grad<MT, JT, WM, WN, HB>), dim3(8 * (unsigned)ceil_div(c.items, 8)),
+  hipLaunchKernelGGL((k_act8_grad<MT, F, WM, WN>), dim3(8 * (unsigned)ceil_div(c.items, 8)),
                      dim3(S::kThreads), 0, s, c);
 }
 
@@ -537,6 +542,7 @@ extern "C" nbsgd_status nbsgd_act_grad(const void* packed, const void* dY, int64
   c.T = T;
   c.dim = dim;
   c.cols = out;
+  c.batches = n * m;
   c.parts = act8_splits(T, dim, out);
   c.per = (int32_t)(ceil_div(ceil_div(lay.blocks, c.parts), 4) * 4);
   c.lay = lay;
@@ -550,9 +556,9 @@ extern "C" nbsgd_status nbsgd_act_grad(const void* packed, const void* dY, int64
   // The largest tile that leaves no CU without one: its products per byte of LDS and of L2 are
   // the most.
   const int64_t each = (int64_t)c.parts * g.count;
-  if (each * ceil_div(dim, 256) * ceil_div(out, 256) >= kTileEnough) grad_launch<2, 4, 8, 1, 4>(c, s);
-  else if (each * ceil_div(dim, 128) * ceil_div(out, 128) >= kTileEnough) grad_launch<4, 1, 2, 2, 2>(c, s);
-  else grad_launch<2, 1, 2, 2, 2>(c, s);
+  if (each * ceil_div(dim, 256) * ceil_div(out, 256) >= kTileEnough) grad_launch<2, 16, 8, 1>(c, s);
+  else if (each * ceil_div(dim, 128) * ceil_div(out, 128) >= kTileEnough) grad_launch<4, 4, 2, 2>(c, s);
+  else grad_launch<2, 4, 2, 2>(c, s);
   if (c.parts > 1)
     hipLaunchKernelGGL(k_act8_parts, dim3((unsigned)std::min<int64_t>(ceil_div(size, 256), 1024), g.count),
                        dim3(256), 0, s, ws, c.parts, size, G, ld, g);
