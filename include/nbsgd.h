@@ -497,8 +497,9 @@ nbsgd_status nbsgd_embed_grad(const void *dY, int64_t ldy, int32_t dtype, int32_
  * states   device fp32 [n][m][batch][ceil(T / NBSGD_SCAN_INTERVAL)][dim], or
  *          NULL: the state before token 0, 256, 512, ...; what the backward
  *          pass needs besides x and g (h itself is not kept for it)
- * workspace  nbsgd_scan_workspace_bytes, for nbsgd_scan and nbsgd_scan_grad
- * n*m*batch*ceil(dim/64) and every row stride are at most 2^22
+ * workspace  nbsgd_scan_workspace_bytes, for nbsgd_scan and nbsgd_scan_grad;
+ *          nbsgd_scan needs none (NULL) for T <= NBSGD_SCAN_INTERVAL
+ * n*m*batch*ceil(dim/64) is at most 2^21 and every row stride at most 2^22
  * (NBSGD_E_UNSUPPORTED).                                                  */
 #define NBSGD_SCAN_INTERVAL 256
 nbsgd_status nbsgd_scan_workspace_bytes(int32_t n, int32_t m, int32_t batch, int32_t T,

@@ -596,7 +596,8 @@ def scan(x, g, mask, h, X=None, offset: int = 0, h0=None, h_last=None, lengths=N
     """The gated recurrence h_t = a h_{t-1} + (1 - a) x_t, a = sigmoid(g + bias), over x, g and h
     [n, m, batch, T, dim] (float32 or bfloat16 rows); the bias [dim] at ``offset`` of row i of
     X [n, ld], or none.  h0 and h_last float32 [n, m, batch, dim] (h_last may be h0), lengths int32
-    [n, m, batch], states float32 [n, m, batch, ceil(T / SCAN_INTERVAL), dim] for the backward pass."""
+    [n, m, batch], states float32 [n, m, batch, ceil(T / SCAN_INTERVAL), dim] for the backward pass.
+    No workspace is needed for T <= SCAN_INTERVAL."""
     f32 = (_torch or _use_torch()).float32
     *args, lens, st = _scan_args(x, g, X, offset, lengths, states)
     n, m, b, T, dim = shape = x.shape

@@ -23,8 +23,8 @@ namespace {
 
 // Gate a = sigmoid(z) and its complement, both accurate where they are small (1 - a would
 // cancel): with e = exp(-|z|) the larger is 1 / (1 + e) and the smaller e / (1 + e).  e is
-// 2^(-|z| log2 e) on the hardware's exponential; EXACT adds what the product's and the
-// constant's rounding lost (|z| 2^-24 of the value otherwise, below bf16's own step).
+// 2^(-|z| log2 e) on the hardware's exponential; EXACT (fp32 rows) adds what the product's and
+// the constant's rounding lost (|z| 2^-24 of the value otherwise, below bf16's own step).
 struct Gate {
   float a, rest;
 };
@@ -38,7 +38,10 @@ __device__ __forceinline__ Gate gate(float z) {
     const float lost = fmaf(y, kLlo, fmaf(y, kL, -t)) * 0.693147181f;
     e = y > -200.f ? fmaf(e, lost, e) : e;
   }
-  const float r = __builtin_amdgcn_rcpf(1.f + e), s = e * r;
+  const float d = 1.f + e;
+  float r = __builtin_amdgcn_rcpf(d);
+  if constexpr (EXACT) r = fmaf(fmaf(-d, r, 1.f), r, r);  // the reciprocal's last place
+  const float s = e * r;
   return z >= 0.f ? Gate{r, s} : Gate{s, r};
 }
 
@@ -366,6 +369,11 @@ __global__ void __launch_bounds__(64 * kScanWaves, 8)
   load_bias<V>(c, w, w.col + o, bias);
   for (int tile = w.chunk * c.chunk; tile < min((w.chunk + 1) * c.chunk, c.tiles); ++tile) {
     const int64_t row = w.seq * c.T + tile * kScanTile + 32 * wave;
+    if (tile * kScanTile >= w.len) {  // uniform: behind the sequence
+      if (wave == 0 && lane < CH && own < c.dim)
+        *reinterpret_cast<f32x2*>(pairs + 2 * ((w.seq * c.tiles + tile) * c.dim + own)) = (f32x2){1.f, 0.f};
+      continue;
+    }
     const bool full = (tile + 1) * kScanTile <= w.len;
     const int live = w.len - tile * kScanTile - 32 * wave - sub * K;
     u32x2 rp[K], rg[K];
@@ -881,12 +889,13 @@ extern "C" nbsgd_status nbsgd_scan(const void* x, const void* g, int64_t ldx, in
   if (((uintptr_t)h0 | (uintptr_t)h_last | (uintptr_t)states | (uintptr_t)lengths) & 3)
     return fail(NBSGD_E_ALIGN, "h0, h_last, states and lengths must be 4-byte aligned");
   const ScanSpace w = scan_space(seqs, T, dim);
-  if (nbsgd_status st = check_workspace(workspace, workspace_bytes, w.total)) return st;
+  const size_t need = T > kScanTile ? w.total : 0;  // a sequence of one tile is not split
+  if (nbsgd_status st = check_workspace(workspace, workspace_bytes, need)) return st;
   const int64_t kept = seqs * dim * 4, all = kept * w.tiles;
   const Rows b[] = {{"h", h, rows, width, ldh * e},
                     {"h_last", h_last, 1, kept, kept},
                     {"states", states, 1, all, all},
-                    {"workspace", workspace, 1, (int64_t)w.total, (int64_t)w.total},
+                    {"workspace", workspace, 1, (int64_t)need, (int64_t)need},
                     {"x", x, rows, width, ldx * e},
                     {"g", g, rows, width, ldx * e},
                     {"h0", h0 == h_last ? nullptr : h0, 1, kept, kept},

@@ -51,6 +51,8 @@ nbsgd_status check_params(const char* name, const void* p, int64_t ld, int64_t p
   if (ld < params || ld % 4)
     return fail(NBSGD_E_SHAPE, "row stride %lld must be a multiple of 4 and hold the %lld floats of %s",
                 (long long)ld, (long long)params, name);
+  if (ld > (int64_t)1 << 40)
+    return fail(NBSGD_E_SHAPE, "row stride %lld of %s exceeds 2^40", (long long)ld, name);
   if (!p) return fail(NBSGD_E_ARG, "%s is null", name);
   if ((uintptr_t)p & 15) return fail(NBSGD_E_ALIGN, "%s must be 16-byte aligned", name);
   return NBSGD_OK;
@@ -107,7 +109,7 @@ nbsgd_status check_scan(int32_t n, int32_t m, int32_t batch, int32_t T, int32_t 
   if (T > NBSGD_MAX_LENGTH || dim > NBSGD_MAX_WIDTH)
     return fail(NBSGD_E_UNSUPPORTED, "T=%d, dim=%d: at most %d, %d", T, dim, NBSGD_MAX_LENGTH,
                 NBSGD_MAX_WIDTH);
-  if ((int64_t)n * m * batch * ceil_div(dim, 64) > (int64_t)1 << 22)
+  if ((int64_t)n * m * batch * ceil_div(dim, 64) > (int64_t)1 << 21)
     return fail(NBSGD_E_UNSUPPORTED, "n=%d, m=%d, batch=%d, dim=%d: too many sequences", n, m, batch,
                 dim);
   return NBSGD_OK;
@@ -135,7 +137,8 @@ nbsgd_status check_act8(int32_t T, int32_t dim) {
 
 int act8_splits(int64_t T, int64_t dim, int64_t out) {
   const int64_t tiles = ceil_div(dim, 64) * ceil_div(out, 128);
-  return (int)std::max<int64_t>(1, std::min(kSplitTiles / tiles, T / kSplitTokens));
+  const int64_t tokens = std::max(kSplitTokens, 12 * dim * out / (dim + 2 * out));
+  return (int)std::max<int64_t>(1, std::min(kSplitTiles / tiles, T / tokens));
 }
 
 size_t act8_space(int64_t groups, int64_t T, int64_t dim, int64_t out) {

@@ -95,7 +95,11 @@ nbsgd_status check_act8(int32_t T, int32_t dim);
 // Parts that the tokens of a weight gradient are summed in, by workgroups of their own where
 // its smallest tiles (64 x 128) are few and the tokens many.  By the mini-batch's sizes alone,
 // not by how many mini-batches a call has, so that a result does not depend on the others.
-constexpr int64_t kSplitTiles = 128, kSplitTokens = 1024;
+// One mini-batch of 16384 x 1024 x 1024: 97 us in four parts, 248 in one.  A part costs a write
+// and a read of the gradient, 8 dim out bytes, so it has the tokens to read half as much again,
+// dim + 2 out bytes each: 16 mini-batches of 4096 x 1024 x 1024 take 143 us in one part and
+// 249 in four, of 8192 x 256 x 256 46 us in eight parts and 73 in two.
+constexpr int64_t kSplitTiles = 512, kSplitTokens = 1024;
 int act8_splits(int64_t T, int64_t dim, int64_t out);
 size_t act8_space(int64_t groups, int64_t T, int64_t dim, int64_t out);
 

@@ -100,7 +100,7 @@ def test_sizes_and_mask(name, change, status):
     ("scan", "ldh", 0, _lib.E_SHAPE), ("scan", "x", None, _lib.E_ARG), ("scan", "g", (1 << 41) + 1, _lib.E_ALIGN),
     ("scan", "h", None, _lib.E_ARG), ("scan", "bias", (1 << 41) + 4, _lib.E_ALIGN), ("scan", "ld", 20, _lib.E_SHAPE),
     ("scan", "h0", (1 << 41) + 2, _lib.E_ALIGN), ("scan", "lengths", (1 << 41) + 1, _lib.E_ALIGN),
-    ("scan", "workspace", None, _lib.E_ARG), ("scan", "workspace_bytes", 8, _lib.E_ARG),
+    ("scan_grad", "workspace", None, _lib.E_ARG), ("scan_grad", "ld", (1 << 41), _lib.E_SHAPE),
     ("scan", "batch", 1 << 21, _lib.E_UNSUPPORTED), ("scan", "ldx", (1 << 22) + 1, _lib.E_UNSUPPORTED),
     ("scan", "ldh", (1 << 22) + 1, _lib.E_UNSUPPORTED), ("scan_grad", "lddh", (1 << 22) + 1, _lib.E_UNSUPPORTED),
     ("scan_grad", "states", None, _lib.E_ARG), ("scan_grad", "dh", None, _lib.E_ARG),
@@ -142,6 +142,12 @@ def test_a_gradient_larger_than_the_memory():
         _lib.E_UNSUPPORTED
 
 
+def test_the_forward_recurrence_of_one_tile_needs_no_workspace():
+    assert _call("scan", T=256, workspace=None, workspace_bytes=0) == _lib.OK
+    assert _call("scan", T=257, workspace=None, workspace_bytes=0) == _lib.E_ARG
+    assert _call("scan", T=257, workspace_bytes=8) == _lib.E_ARG
+
+
 def test_rows_side_by_side_do_not_overlap():
     p = 1 << 42
     assert _call("scan_grad", ldx=48, dx=p, dg=p + 48) == _lib.OK
@@ -167,7 +173,7 @@ def test_sizes():
     assert nb.act_bytes(262144, 65536) == 8192 * 65536 * 32 + 2048 * 65536 * 4
     assert nb.scan_workspace_bytes(1, 1, 1, 0, 8) == 0
     for call, args in ((nb.embed_workspace_bytes, (16, 64, 262144, 1 << 24, 65536)),
-                       (nb.scan_workspace_bytes, (16, 64, 4, 1 << 24, 65536)),
+                       (nb.scan_workspace_bytes, (16, 64, 2, 1 << 24, 65536)),
                        (nb.act_workspace_bytes, (16, 64, 262144, 65536, 65536))):
         assert call(*args) >= 0
     for call, args in ((nb.act_bytes, (-1, 4)), (nb.embed_workspace_bytes, (1, 1, 1, 0, 4)),
