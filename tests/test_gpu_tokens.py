@@ -364,6 +364,112 @@ def test_act_grad(n, m, T, dim, out, gap, shift):
     assert (G[:, :, :offset] == SENTINEL).all() and (G[:, :, offset + dim * out:] == SENTINEL).all()
 
 
+# ---------------------------------------------- far rows, states in place
+def test_rows_beyond_32_bits():
+    """Rows so far apart that byte offsets pass 2^32, and a table of more than 2^31 floats."""
+    rng = np.random.default_rng(2)
+    T, C, far = 520, 72, 1 << 22
+    _say("scan, rows 2^22 apart")
+    xg = torch.empty((1, 1, 1, T, far), dtype=BF16, device=DEV)
+    dxg = torch.empty((1, 1, 1, T, far), dtype=BF16, device=DEV)
+    near = _rows((2, T, C), BF16, rng=rng)[0].contiguous()
+    x, g, dx, dg = (t[..., o:o + C] for t in (xg, dxg) for o in (0, far // 2))
+    x.copy_(near[0]), g.copy_(near[1])
+    h = torch.empty((1, 1, 1, T, C), dtype=BF16, device=DEV)
+    dh = _rows(h.shape, BF16, rng=rng)[0].contiguous()
+    st = torch.empty((1, 1, 1, 3, C), device=DEV)
+    ws = _ws(nb.scan_workspace_bytes(1, 1, 1, T, C))
+    nb.scan(x, g, [[1]], h, states=st, workspace=ws)
+    nb.scan_grad(x, g, st, dh, [[1]], dx, dg, ws)
+    v = _np(near)
+    (ho, _, _), (eh, _, _) = orc.scan(v[0], v[1], np.zeros(C), np.zeros(C), T)
+    (gx, gg, _, _), (ex, eg, _, _) = orc.scan_grad(v[0], v[1], np.zeros(C), np.zeros(C), T, _np(dh[0, 0, 0]), np.zeros(C))
+    _close("h", h[0, 0, 0], ho, eh, BF16)
+    _close("dx", dx[0, 0, 0], gx, ex, BF16)
+    _close("dg", dg[0, 0, 0], gg, eg, BF16)
+    del xg, dxg, x, g, dx, dg
+
+    V, D = (1 << 20) + 5, 2100
+    _say("embed, a table of 2.2e9 floats")
+    X = torch.empty((1, V * D), device=DEV)
+    tok = np.array([V - 1, 0, V - 3, V - 1, -1, V], np.int32)
+    for t in (0, V - 3, V - 1):
+        X[0, t * D:(t + 1) * D] = torch.from_numpy(rng.normal(size=D).astype(np.float32)).to(DEV)
+    tokens = torch.from_numpy(tok).to(DEV).view(1, 1, 6)
+    Y = torch.empty((1, 1, 6, D), device=DEV)
+    nb.embed(X, 0, V, tokens, [[1]], Y)
+    for k, t in enumerate(tok[:4]):
+        assert torch.equal(Y[0, 0, k], X[0, int(t) * D:(int(t) + 1) * D])
+    assert (Y[0, 0, 4:] == 0).all()
+    for T in (6, 150):  # few tokens, and sorted ones
+        X.fill_(SENTINEL)
+        many = torch.full((1, 1, T), -1, dtype=torch.int32, device=DEV)
+        many[0, 0, :6] = tokens[0, 0]
+        dY = _rows((1, 1, T, D), F32, rng=rng)[0].contiguous()
+        nb.embed_grad(dY, many, [[1]], X.view(1, 1, -1), 0, V, _ws(nb.embed_workspace_bytes(1, 1, T, V, D)))
+        assert torch.equal(X[0, (V - 1) * D:], dY[0, 0, 0] + dY[0, 0, 3])
+        assert torch.equal(X[0, :D], dY[0, 0, 1]) and torch.equal(X[0, (V - 3) * D:(V - 2) * D], dY[0, 0, 2])
+        assert int(torch.count_nonzero(X)) == sum(int(torch.count_nonzero(t)) for t in (
+            X[0, (V - 1) * D:], X[0, :D], X[0, (V - 3) * D:(V - 2) * D]))
+    del X
+
+    T, D, N = 300, 40, 24
+    _say("act_grad, rows 2^22 apart")
+    wide = torch.empty((1, 2, T, far), dtype=BF16, device=DEV)
+    dY = wide[..., far - N:]
+    dY.copy_(_rows((1, 2, T, N), BF16, rng=rng)[0])
+    A = torch.empty((1, 2, T, far), dtype=BF16, device=DEV)[..., far - D:]
+    A.copy_(_rows((1, 2, T, D), BF16, rng=rng)[0])
+    packed = torch.empty((1, 2, nb.act_bytes(T, D)), dtype=torch.uint8, device=DEV)
+    G = torch.empty((1, 2, D * N), device=DEV)
+    nb.act_pack(A, [[1, 1]], packed)
+    nb.act_grad(packed, dY, [[1, 1]], G, 0, D, _ws(nb.act_workspace_bytes(1, 2, T, D, N)))
+    q, step = orc.act8(_np(A[0, 1]))
+    want, bound = orc.act_grad(q * step, _np(dY[0, 1]))
+    _close("G", G[0, 1].view(D, N), want, bound)
+    A.fill_(SENTINEL)
+    nb.act_unpack(packed, [[0, 1]], A)
+    assert np.array_equal(_np(A[0, 1]), q * step) and (A[0, 0] == SENTINEL).all()
+
+
+@pytest.mark.parametrize("T,C", [(16, 20), (200, 70), (700, 33), (3000, 130)])
+def test_states_in_place(T, C):
+    """h_last over h0 and dh0 over dh_last, in one tile and split over workgroups."""
+    rng = np.random.default_rng(T)
+    d = _scan_inputs(rng, 1, 2, 1, T, C, 0, "ragged", 1, 1, F32)
+    mask = [[1, 1]]
+    h, _, last, st = _scan_call(d, mask, 1, 2, 1, T, C, F32)
+    state, h2 = d["h0"].clone(), torch.empty_like(h)
+    ws = _ws(nb.scan_workspace_bytes(1, 2, 1, T, C))
+    nb.scan(d["x"], d["g"], mask, h2, X=d["X"], offset=4, h0=state, h_last=state, lengths=d["lengths"], workspace=ws)
+    assert torch.equal(h2, h) and torch.equal(state, last)
+    dh = _rows(h.shape, F32, rng=rng)[0].contiguous()
+    out = []
+    for same in (False, True):
+        dl = torch.linspace(-1, 1, 2 * C, device=DEV).view(1, 2, 1, C).contiguous()
+        dx, _ = _rows(h.shape, F32, 3, 1)
+        dg, _ = _rows(h.shape, F32, 3, 2)
+        d0 = dl if same else torch.empty_like(dl)
+        nb.scan_grad(d["x"], d["g"], st, dh, mask, dx, dg, ws, X=d["X"], offset=4, dh_last=dl, dh0=d0, lengths=d["lengths"])
+        out.append((dx.clone(), dg.clone(), d0))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+def test_infinite_bias_and_empty_sequences():
+    """A bias of -inf passes x through, one of +inf keeps the state; where a sequence has ended the state
+    stays whatever the bias is."""
+    T, C = 600, 3
+    X = torch.tensor([[0.0, 0, 0, 0, -float("inf"), float("inf"), 0.0, 0]], device=DEV)
+    x, g = torch.full((1, 1, 2, T, C), 3.0, device=DEV), torch.zeros((1, 1, 2, T, C), device=DEV)
+    h0 = torch.full((1, 1, 2, C), 5.0, device=DEV)
+    h, last = torch.empty_like(x), torch.empty_like(h0)
+    lengths = torch.tensor([[[0, 300]]], dtype=torch.int32, device=DEV)
+    nb.scan(x, g, [[1]], h, X=X, offset=4, h0=h0, h_last=last, lengths=lengths,
+            workspace=_ws(nb.scan_workspace_bytes(1, 1, 2, T, C)))
+    assert (last[0, 0, 0] == 5).all() and (h[0, 0, 0] == 0).all()
+    assert last[0, 0, 1].tolist() == [3.0, 5.0, 3.0] and (h[0, 0, 1, 300:] == 0).all()
+
+
 # ------------------------------------------------------------- all of them
 def _one_pass(d, mask, sel=None):
     """Every call on the mini-batches of `mask`; the outputs by name.  `sel`: only mini-batch
