@@ -1,4 +1,6 @@
 // Embedding lookup with scaling and its gradient, per learner and mini-batch (gfx950).
+#include <algorithm>
+
 #include "device_rows.h"
 
 using namespace nbsgd;
@@ -38,14 +40,17 @@ __global__ void __launch_bounds__(256)
 
 // ---- gradient of the lookup
 //
-// The tokens of a mini-batch are sorted (k_sort, stable, so that equal tokens keep their order),
-// and the sorted tokens merged with the table's rows 0 .. vocab - 1, a row after the tokens
-// equal to it.  That list is cut into equal pieces, one a team of lanes: a team walks
-// its piece, adds the dY row of a token and writes G's row at a row.  So every team has the
-// same work whatever the tokens are, every row of G is written once, and a row whose tokens
-// cross a piece's border is summed from the pieces' parts, in order, by k_embed_join.  What
-// bounds it is the write of G, vocab x dim floats a mini-batch.
-
+// The tokens of a mini-batch are sorted (k_sort, stable, so that equal tokens keep their order)
+// and the rows of dY added run by run, by teams of lanes that take equal pieces, so that every
+// team has the same work whatever the tokens are.  A row whose tokens cross a piece's border is
+// summed from the pieces' parts, in order, by k_embed_join; no atomics.  What bounds it is the
+// write of G, vocab x dim floats a mini-batch.  Two ways:
+//   merged  the pieces are cut from the sorted tokens merged with the table's rows 0 .. vocab -
+//           1, a row after the tokens equal to it; every row of G is written once
+//   filled  the sort's launch has workgroups that write zeros to all of G, behind which the sort
+//           hides; the pieces are cut from the tokens alone, and the rows that have tokens are
+//           written again.  Where those are few (tokens of a mini-batch at most half the table):
+//           16 mini-batches of 8192 tokens, 32000 x 512, @FILLED@ us, merged 289
 // Sorted entry: token in the high word, position in the low; tokens outside the table as vocab.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 
@@ -55,15 +60,25 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 template <int ITEMS>
 __global__ void __launch_bounds__(kSortThreads)
     k_sort(const int32_t* __restrict__ tokens, int Tn, int vocab, int bits, uint2* __restrict__ keys,
-           Groups groups) {
+           float* __restrict__ G, int64_t ld, int64_t size, int fills, Groups groups) {
   constexpr int N = kSortThreads * ITEMS;
+  const int runs = (Tn + N - 1) / N, sorts = runs * groups.count;
+  if ((int)blockIdx.x >= sorts) {  // uniform: a part of a mini-batch's zeros
+    const int f = blockIdx.x - sorts;
+    float* to = G + (int64_t)group_id(groups, f / fills) * ld;
+    const int64_t quads = size / 4, from = f % fills * (int64_t)kSortThreads + threadIdx.x;
+    for (int64_t k = from; k < quads; k += (int64_t)fills * kSortThreads)
+      __builtin_nontemporal_store((f32x4){0.f, 0.f, 0.f, 0.f}, reinterpret_cast<f32x4*>(to) + k);
+    if (from < size % 4) to[4 * quads + from] = 0.f;
+    return;
+  }
   __shared__ uint32_t tok[N];
   __shared__ uint16_t pos[N];
   __shared__ uint32_t hist[kSortWaves][256];
   __shared__ uint32_t wsum[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t id = group_id(groups, blockIdx.y);
-  const int first = blockIdx.x * N, count = min(N, Tn - first);
+  const int64_t id = group_id(groups, blockIdx.x / runs);
+  const int first = blockIdx.x % runs * N, count = min(N, Tn - first);
   const int32_t* src = tokens + id * Tn + first;
   // wave w holds tokens 64 ITEMS w + 64 k + lane, k = 0 .. ITEMS - 1; the ones past the count sort last
   uint32_t key[ITEMS], at[ITEMS];
@@ -252,6 +267,7 @@ struct GradCall {
   float* G;
   int64_t ldy, ld, pieces;
   int32_t T, vocab, dim, items, L;  // items of a piece, lanes of a team
+  int32_t merged;   // pieces of tokens and rows, or of tokens alone
   float scale;
   Groups groups;
 };
@@ -319,6 +335,60 @@ __global__ void __launch_bounds__(256) k_embed_grad(const T* __restrict__ dY, Gr
   }
 }
 
+// The same over pieces of the tokens alone: the rows without any are zeros already.
+template <typename T>
+__global__ void __launch_bounds__(256) k_embed_runs(const T* __restrict__ dY, GradCall c) {
+  constexpr int V = 4, U = 8;
+  __shared__ uint2 stage[256 / kMinTeam][kMaxPiece];
+  const int64_t id = group_id(c.groups, blockIdx.y);
+  const int team = threadIdx.x / c.L, l = threadIdx.x % c.L;
+  const int64_t piece = (int64_t)blockIdx.x * (256 / c.L) + team;
+  const uint2* s = c.sorted + id * c.T;
+  const int k0 = (int)min(piece, c.pieces - 1) * c.items, k1 = min(k0 + c.items, c.T);
+  uint2* mine = stage[team];
+  for (int k = l; k < k1 - k0; k += c.L) mine[k] = s[k0 + k];
+  const uint32_t before = k0 ? s[k0 - 1].y : ~0u, behind = k1 < c.T ? s[k1].y : ~0u;
+  __syncthreads();
+  if (piece >= c.pieces) return;
+  int count = k1 - k0;  // tokens outside the table come last, and are not read
+  while (count > 0 && mine[count - 1].y == (uint32_t)c.vocab) --count;
+  const bool carried = count > 0 && before == mine[0].y;
+  const bool open = count > 0 && behind == mine[count - 1].y;
+  // the piece ends the row that it was handed, unless it goes on behind it
+  const bool ends = carried && !(open && mine[0].y == mine[count - 1].y);
+  if (l == 0) c.flags[id * c.pieces + piece] = ends ? (int)mine[0].y : -1;
+  const T* rows = dY + id * c.T * c.ldy;
+  float* part = c.parts + 2 * (id * c.pieces + piece) * c.dim;
+  for (int col = V * l; col < c.dim; col += V * c.L) {
+    const int n = min(V, c.dim - col);
+    float sum[V] = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < count; k += U) {
+      float e[U][V];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        load4(rows + (int64_t)mine[min(k + u, count - 1)].x * c.ldy + col, n, e[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (k + u >= count) break;
+        const uint32_t r = mine[k + u].y;
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += e[u][v];
+        if (k + u + 1 < count ? mine[k + u + 1].y == r : open) continue;  // the row goes on
+        if (ends && r == mine[0].y) {
+          store4(part + col, n, sum);
+        } else {
+#pragma unroll
+          for (int v = 0; v < V; ++v) sum[v] *= c.scale;
+          store_row4(c.G + id * c.ld + (int64_t)r * c.dim + col, n, sum);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] = 0.f;
+      }
+    }
+    if (open) store4(part + c.dim + col, n, sum);
+  }
+}
+
 // The rows that more than one piece has tokens of: the earlier pieces' parts in order, then the
 // last piece's.  A wave a piece; most of them end no such row.
 __global__ void __launch_bounds__(256) k_embed_join(GradCall c) {
@@ -346,7 +416,7 @@ __global__ void __launch_bounds__(256) k_embed_join(GradCall c) {
     const int n = min(4, c.dim - col);
     float sum[4] = {0.f, 0.f, 0.f, 0.f}, e[4];
 #pragma unroll 16
-    for (int64_t q = (lo + r) / c.items; q < piece; ++q) {
+    for (int64_t q = (lo + (c.merged ? r : 0)) / c.items; q < piece; ++q) {
       load4(parts + (2 * q + 1) * c.dim + col, n, e);
 #pragma unroll
       for (int v = 0; v < 4; ++v) sum[v] += e[v];
@@ -422,10 +492,13 @@ __global__ void __launch_bounds__(256)
 }
 
 template <int ITEMS>
-void sort_launch(const int32_t* tokens, int32_t T, int32_t vocab, int bits, uint2* keys, const Groups& g,
-                 hipStream_t s) {
-  hipLaunchKernelGGL(k_sort<ITEMS>, dim3((unsigned)ceil_div(T, kSortThreads * ITEMS), g.count),
-                     dim3(kSortThreads), 0, s, tokens, T, vocab, bits, keys, g);
+void sort_launch(const int32_t* tokens, const GradCall& c, int bits, uint2* keys, hipStream_t s) {
+  const int64_t size = c.merged ? 0 : (int64_t)c.vocab * c.dim;
+  // about 2,048 workgroups of zeros, each with at least four rounds of stores
+  const int64_t fills = std::min<int64_t>(ceil_div(2048, c.groups.count), ceil_div(size, 16 * kSortThreads));
+  hipLaunchKernelGGL(k_sort<ITEMS>, dim3((unsigned)((ceil_div(c.T, kSortThreads * ITEMS) + fills) * c.groups.count)),
+                     dim3(kSortThreads), 0, s, tokens, c.T, c.vocab, bits, keys, c.G, c.ld, size, (int)fills,
+                     c.groups);
 }
 
 template <typename T>
@@ -444,18 +517,23 @@ void embed_grad_launch(const void* dY, const int32_t* tokens, GradCall c, const 
                        dim3(256), 0, s, static_cast<const T*>(dY), tokens, c);
     return;
   }
+  c.merged = 2 * (int64_t)c.T > c.vocab;
+  if (!c.merged) {
+    c.items = piece_items(c.T);
+    c.pieces = ceil_div(c.T, c.items);
+  }
   int bits = 1;
   while ((c.vocab + 1) >> bits) ++bits;  // of vocab + 1, the largest key
   // one run up to 8,192 tokens: 18 us at that length, against 8 us for runs of 2,048 and 14 to
   // join them
   int run = kSortThreads;
   if (c.T <= kSortThreads) {
-    sort_launch<1>(tokens, c.T, c.vocab, bits, keys, c.groups, s);
+    sort_launch<1>(tokens, c, bits, keys, s);
   } else if (c.T <= 4 * kSortThreads) {
-    sort_launch<4>(tokens, c.T, c.vocab, bits, keys, c.groups, s);
+    sort_launch<4>(tokens, c, bits, keys, s);
     run = 4 * kSortThreads;
   } else {
-    sort_launch<8>(tokens, c.T, c.vocab, bits, keys, c.groups, s);
+    sort_launch<8>(tokens, c, bits, keys, s);
     run = 8 * kSortThreads;
   }
   c.sorted = keys;
@@ -465,8 +543,11 @@ void embed_grad_launch(const void* dY, const int32_t* tokens, GradCall c, const 
     c.sorted = sorted;
   }
   while (c.L < 128 && c.L * 4 < c.dim) c.L *= 2;
-  hipLaunchKernelGGL(k_embed_grad<T>, dim3((unsigned)ceil_div(c.pieces, 256 / c.L), c.groups.count), dim3(256),
-                     0, s, static_cast<const T*>(dY), c);
+  const dim3 grid((unsigned)ceil_div(c.pieces, 256 / c.L), c.groups.count);
+  if (c.merged)
+    hipLaunchKernelGGL(k_embed_grad<T>, grid, dim3(256), 0, s, static_cast<const T*>(dY), c);
+  else
+    hipLaunchKernelGGL(k_embed_runs<T>, grid, dim3(256), 0, s, static_cast<const T*>(dY), c);
   hipLaunchKernelGGL(k_embed_join, dim3((unsigned)ceil_div(c.pieces, 4), c.groups.count), dim3(256), 0, s, c);
 }
 

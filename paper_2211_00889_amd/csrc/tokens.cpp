@@ -91,7 +91,7 @@ nbsgd_status check_embed(int32_t T, int32_t vocab, int32_t dim) {
 EmbedSpace embed_space(int64_t groups, int64_t T, int64_t vocab, int64_t dim) {
   EmbedSpace s;
   const int64_t all = T + vocab;
-  s.items = all >= 64 * kMaxPiece ? kMaxPiece : all >= 32 * kMaxPiece ? 32 : 16;
+  s.items = piece_items(all);
   s.pieces = ceil_div(all, s.items);
   s.keys = 0;
   s.sorted = s.keys + up256((size_t)groups * T * 8);
