@@ -90,8 +90,12 @@ nbsgd_status check_embed(int32_t T, int32_t vocab, int32_t dim) {
 
 EmbedSpace embed_space(int64_t groups, int64_t T, int64_t vocab, int64_t dim) {
   EmbedSpace s;
-  const int64_t all = T + vocab;
-  s.items = piece_items(all);
+  s.merged = 2 * T > vocab;
+  const int64_t all = s.merged ? T + vocab : T;
+  // tokens alone: 32 of them (16 mini-batches of 8192 x 512: 264 us, 16 tokens 267, 64 tokens 272);
+  // merged, a piece has rows without tokens too, and takes 64 entries.  Fewer where a mini-batch
+  // is small and the time is a piece's own
+  s.items = all < 32 * 64 ? 16 : !s.merged || all < 64 * 64 ? 32 : kMaxPiece;
   s.pieces = ceil_div(all, s.items);
   s.keys = 0;
   s.sorted = s.keys + up256((size_t)groups * T * 8);

@@ -56,16 +56,13 @@ nbsgd_status check_workspace(const void* ws, size_t bytes, size_t need);
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// ---- embeddings: the list of a mini-batch's sorted tokens, merged with the table's rows, is cut
-// into pieces (embed.hip): of 64 entries, where that gives a mini-batch at least 64 of them,
-// of 16 or 32 where it is small and the time is a piece's own
+// ---- embeddings: pieces of the gradient's work (embed.hip), cut from a mini-batch's sorted tokens
+// merged with the table's rows, or from the tokens alone
 constexpr int kMaxPiece = 64;
-inline int32_t piece_items(int64_t all) {
-  return all >= 64 * kMaxPiece ? kMaxPiece : all >= 32 * kMaxPiece ? 32 : 16;
-}
 struct EmbedSpace {
-  int64_t pieces;     // of one mini-batch
+  bool merged;
   int32_t items;      // of a piece
+  int64_t pieces;     // of one mini-batch
   size_t keys, sorted, flags, parts, total;  // byte offsets, and the whole
 };
 EmbedSpace embed_space(int64_t groups, int64_t T, int64_t vocab, int64_t dim);

@@ -141,6 +141,25 @@ def test_embed_grad(kind, n, m, T, vocab, dim, gap, shift, dtype):
     assert (G[:, :, :offset] == SENTINEL).all() and (G[:, :, offset + vocab * dim:] == SENTINEL).all()
 
 
+@pytest.mark.parametrize("T", [129, 700, 1023, 1024, 1500, 2047, 2048, 4100])
+@pytest.mark.parametrize("rows", [-1, 0, 1, 37])  # of the table, beside twice the tokens
+def test_embed_grad_keeps_to_its_workspace(T, rows):
+    """Where the pieces' number changes with the sizes: nothing behind the stated bytes is written."""
+    n, m, vocab, dim = 2, 1, 2 * T + rows, 20
+    rng = np.random.default_rng(T)
+    _say(f"embed_grad T={T} vocab={vocab}")
+    tok = _tokens(rng, "zipf", (n, m, T), vocab)
+    dY, _ = _rows((n, m, T, dim), F32, rng=rng)
+    G = torch.full((n, m, vocab * dim), SENTINEL, device=DEV)
+    size = nb.embed_workspace_bytes(n, m, T, vocab, dim)
+    guard = torch.full((size + 65536,), 7, dtype=torch.uint8, device=DEV)
+    nb.embed_grad(dY, torch.from_numpy(tok).to(DEV), np.ones((n, m), np.uint8), G, 0, vocab, guard[:size])
+    assert (guard[size:] == 7).all()
+    for i in range(n):
+        want, bound = orc.embed_grad(_np(dY[i, 0]), tok[i, 0], vocab, 1.0)
+        _close("G", G[i, 0].view(vocab, dim), want, bound)
+
+
 # ------------------------------------------------------------------ recurrence
 SCAN = [
     # n, m, batch, T, dim, joint, lengths, bias, h0
