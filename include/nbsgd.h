@@ -466,9 +466,8 @@ nbsgd_status nbsgd_embed(const float *E, int64_t ld, int32_t n, int32_t m, int32
 
 /* Gradient of the lookup, every row of the table written:
  *   G[i][j][v][:] = scale * sum_{t : tokens[i][j][t] == v} dY[i][j][t][:]
- * The tokens are sorted first, so that a row's sum runs over its own tokens in
- * their order and needs no atomics.  Rows of dY whose token lies outside
- * [0, vocab) are not read.
+ * A row's sum runs over its own tokens in an order that the tokens alone fix; no
+ * atomics.  Rows of dY whose token lies outside [0, vocab) are not read.
  * G  device fp32, the gradient of mini-batch (i, j) at G + (i*m + j)*ld
  * workspace  nbsgd_embed_workspace_bytes(n, m, T, vocab, dim)             */
 nbsgd_status nbsgd_embed_workspace_bytes(int32_t n, int32_t m, int32_t T, int32_t vocab,

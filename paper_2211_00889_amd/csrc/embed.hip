@@ -41,16 +41,14 @@ __global__ void __launch_bounds__(256)
 // ---- gradient of the lookup
 //
 // The tokens of a mini-batch are sorted (k_sort, stable, so that equal tokens keep their order)
-// and the rows of dY added run by run, by teams of lanes that take equal pieces, so that every
-// team has the same work whatever the tokens are.  A row whose tokens cross a piece's border is
-// summed from the pieces' parts, in order, by k_embed_join; no atomics.  What bounds it is the
-// write of G, vocab x dim floats a mini-batch.  Two ways:
-//   merged  the pieces are cut from the sorted tokens merged with the table's rows 0 .. vocab -
-//           1, a row after the tokens equal to it; every row of G is written once
-//   filled  the sort's launch has workgroups that write zeros to all of G, behind which the sort
-//           hides; the pieces are cut from the tokens alone, and the rows that have tokens are
-//           written again.  Where those are few (tokens of a mini-batch at most half the table):
-//           16 mini-batches of 8192 tokens, 32000 x 512, 264 us, merged 289
+// and the rows of dY added run by run, by teams of lanes that take equal pieces of the sorted
+// tokens, so that every team has the same work whatever the tokens are.  A row whose tokens
+// cross a piece's border is summed from the pieces' parts, in order, by k_embed_join; no atomics.
+// What bounds it is the write of G, vocab x dim floats a mini-batch: workgroups beside the sort
+// write zeros to all of it, and hide it, and the rows that have tokens are written again.  (With
+// pieces of the tokens merged with the table's rows each row is written once, but after the sort:
+// 16 x 8192 tokens, 32000 x 512, 289 against 264 us; with as many tokens as rows 125 against 115,
+// with 16 times as many 106 against 108.)
 // Sorted entry: token in the high word, position in the low; tokens outside the table as vocab.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 
@@ -191,50 +189,6 @@ __global__ void __launch_bounds__(256)
   sorted[id * Tn + to] = e;
 }
 
-// Tokens among the first d0 (d1) entries of the merged list of `count` sorted tokens and the
-// rows: token k is entry k + (its token), the rows before it.  Sixteen lanes probe at a time, so
-// that a step leaves a seventeenth (8,192 tokens in four dependent loads, not thirteen), and
-// both searches share the steps.
-__device__ __forceinline__ void tokens_before(const uint2* s, int count, int vocab, int d0, int d1, int* k0,
-                                              int* k1) {
-  const int l = threadIdx.x & 15, base = threadIdx.x & 48;
-  int d[2] = {d0, d1}, lo[2], hi[2];
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    lo[q] = max(0, d[q] - vocab);
-    hi[q] = min(d[q], count);
-  }
-  while (__any(lo[0] < hi[0] || lo[1] < hi[1])) {
-    int probe[2];
-    uint32_t tok[2];
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      // 16 places of [lo, hi), ascending; all of a short range, its last one over and over
-      const int n = hi[q] - lo[q];
-      probe[q] = n <= 16 ? min(lo[q] + l, hi[q] - 1) : lo[q] + (int)((int64_t)n * (l + 1) / 17);
-      tok[q] = n > 0 ? s[probe[q]].y : 0u;
-    }
-    int c[2];  // probes 0 .. c - 1 are in
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const bool in = hi[q] > lo[q] && (int)tok[q] <= d[q] - 1 - probe[q];
-      c[q] = __builtin_popcount((uint32_t)(__ballot(in) >> base) & 0xffffu);
-    }
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int n = hi[q] - lo[q], from = lo[q];
-      if (n <= 16) {
-        lo[q] = hi[q] = from + min(c[q], max(n, 0));
-      } else {
-        if (c[q]) lo[q] = from + (int)((int64_t)n * c[q] / 17) + 1;
-        if (c[q] < 16) hi[q] = from + (int)((int64_t)n * (c[q] + 1) / 17);
-      }
-    }
-  }
-  *k0 = lo[0];
-  *k1 = lo[1];
-}
-
 // The first n (at most 4) elements at p, zeros behind them; and back.
 __device__ __forceinline__ void load4(const float* p, int n, float (&v)[4]) {
   Elem<float>::expand(load16<float>(p, n), v);
@@ -267,8 +221,7 @@ struct GradCall {
   float* parts;     // per piece: that row's share of the piece, and the piece's share of the row it leaves
   float* G;
   int64_t ldy, ld, pieces;
-  int32_t T, vocab, dim, items, L;  // items of a piece, lanes of a team
-  int32_t merged;   // pieces of tokens and rows, or of tokens alone
+  int32_t T, vocab, dim, items, L;  // tokens of a piece, lanes of a team
   float scale;
   Groups groups;
 };
@@ -276,69 +229,6 @@ struct GradCall {
 // A team a piece: its entries to LDS, then the rows of dY in their order, U of them under way.
 template <typename T>
 __global__ void __launch_bounds__(256) k_embed_grad(const T* __restrict__ dY, GradCall c) {
-  constexpr int V = 4, U = 8;
-  __shared__ uint2 stage[256 / kMinTeam][kMaxPiece + U];
-  const int64_t id = group_id(c.groups, blockIdx.y);
-  const int team = threadIdx.x / c.L, l = threadIdx.x % c.L;
-  // teams past the last piece take it once more and store nothing
-  const int64_t want = (int64_t)blockIdx.x * (256 / c.L) + team;
-  const int64_t piece = min(want, c.pieces - 1);
-  const uint2* s = c.sorted + id * c.T;
-  const int d0 = (int)piece * c.items, d1 = min(d0 + c.items, c.T + c.vocab);
-  int k0, k1;
-  tokens_before(s, c.T, c.vocab, d0, d1, &k0, &k1);
-  const int r0 = d0 - k0, r1 = d1 - k1;  // rows of the piece; row r1 is left open
-  uint2* mine = stage[team];
-  for (int k = l; k < k1 - k0; k += c.L) mine[k] = s[k0 + k];
-  const bool carried = k0 > 0 && r0 < c.vocab && s[k0 - 1].y == (uint32_t)r0;
-  __syncthreads();
-  if (want != piece) return;
-  if (l == 0) c.flags[id * c.pieces + piece] = carried && r0 < r1 ? r0 : -1;
-  int count = k1 - k0;
-  if (r1 == c.vocab)  // tokens outside the table come last, and are not read
-    while (count > 0 && mine[count - 1].y == (uint32_t)c.vocab) --count;
-  const T* rows = dY + id * c.T * c.ldy;
-  float* part = c.parts + 2 * (id * c.pieces + piece) * c.dim;
-  for (int col = V * l; col < c.dim; col += V * c.L) {
-    const int n = min(V, c.dim - col);
-    float* to = c.G + id * c.ld + (int64_t)r0 * c.dim + col;
-    float sum[V] = {0.f, 0.f, 0.f, 0.f};
-    int r = r0;
-    auto end_row = [&]() {
-      if (r == r0 && carried) {
-        store4(part + col, n, sum);
-      } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] *= c.scale;
-        store_row4(to, n, sum);
-      }
-#pragma unroll
-      for (int v = 0; v < V; ++v) sum[v] = 0.f;
-      to += c.dim;
-      ++r;
-    };
-    for (int k = 0; k < count; k += U) {
-      float e[U][V];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        load4(rows + (int64_t)mine[min(k + u, count - 1)].x * c.ldy + col, n, e[u]);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (k + u >= count) break;
-        while (r < (int)mine[k + u].y) end_row();
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] += e[u][v];
-      }
-    }
-    while (r < r1) end_row();
-    // left open: what the piece has of it
-    if (r1 < c.vocab && count > 0 && mine[count - 1].y == (uint32_t)r1) store4(part + c.dim + col, n, sum);
-  }
-}
-
-// The same over pieces of the tokens alone: the rows without any are zeros already.
-template <typename T>
-__global__ void __launch_bounds__(256) k_embed_runs(const T* __restrict__ dY, GradCall c) {
   constexpr int V = 4, U = 8;
   __shared__ uint2 stage[256 / kMinTeam][kMaxPiece];
   const int64_t id = group_id(c.groups, blockIdx.y);
@@ -417,7 +307,7 @@ __global__ void __launch_bounds__(256) k_embed_join(GradCall c) {
     const int n = min(4, c.dim - col);
     float sum[4] = {0.f, 0.f, 0.f, 0.f}, e[4];
 #pragma unroll 16
-    for (int64_t q = (lo + (c.merged ? r : 0)) / c.items; q < piece; ++q) {
+    for (int64_t q = lo / c.items; q < piece; ++q) {
       load4(parts + (2 * q + 1) * c.dim + col, n, e);
 #pragma unroll
       for (int v = 0; v < 4; ++v) sum[v] += e[v];
@@ -494,7 +384,7 @@ __global__ void __launch_bounds__(256)
 
 template <int ITEMS>
 void sort_launch(const int32_t* tokens, const GradCall& c, int bits, uint2* keys, hipStream_t s) {
-  const int64_t size = c.merged ? 0 : (int64_t)c.vocab * c.dim;
+  const int64_t size = (int64_t)c.vocab * c.dim;
   // about 2,048 workgroups of zeros, each with at least four rounds of stores
   const int64_t fills = std::min<int64_t>(ceil_div(2048, c.groups.count), ceil_div(size, 16 * kSortThreads));
   hipLaunchKernelGGL(k_sort<ITEMS>, dim3((unsigned)((ceil_div(c.T, kSortThreads * ITEMS) + fills) * c.groups.count)),
@@ -509,7 +399,6 @@ void embed_grad_launch(const void* dY, const int32_t* tokens, GradCall c, const 
   uint2* sorted = reinterpret_cast<uint2*>(static_cast<char*>(ws) + w.sorted);
   c.flags = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + w.flags);
   c.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + w.parts);
-  c.merged = w.merged;
   c.pieces = w.pieces;
   c.items = w.items;
   c.L = kMinTeam;
@@ -541,10 +430,7 @@ void embed_grad_launch(const void* dY, const int32_t* tokens, GradCall c, const 
   }
   while (c.L < 128 && c.L * 4 < c.dim) c.L *= 2;
   const dim3 grid((unsigned)ceil_div(c.pieces, 256 / c.L), c.groups.count);
-  if (c.merged)
-    hipLaunchKernelGGL(k_embed_grad<T>, grid, dim3(256), 0, s, static_cast<const T*>(dY), c);
-  else
-    hipLaunchKernelGGL(k_embed_runs<T>, grid, dim3(256), 0, s, static_cast<const T*>(dY), c);
+  hipLaunchKernelGGL(k_embed_grad<T>, grid, dim3(256), 0, s, static_cast<const T*>(dY), c);
   hipLaunchKernelGGL(k_embed_join, dim3((unsigned)ceil_div(c.pieces, 4), c.groups.count), dim3(256), 0, s, c);
 }
 
@@ -599,7 +485,7 @@ extern "C" nbsgd_status nbsgd_embed_grad(const void* dY, int64_t ldy, int32_t dt
   if (nbsgd_status st = check_rows("dY", dY, rows, dim, ldy, e)) return st;
   if (nbsgd_status st = check_rows("tokens", tokens, rows, 1, 1, 4)) return st;
   if (nbsgd_status st = check_params("G", G, ld, (int64_t)vocab * dim)) return st;
-  const EmbedSpace w = embed_space((int64_t)n * m, T, vocab, dim);
+  const EmbedSpace w = embed_space((int64_t)n * m, T, dim);
   if (nbsgd_status st = check_workspace(workspace, workspace_bytes, w.total)) return st;
   const Rows b[] = {{"G", G, (int64_t)n * m, (int64_t)vocab * dim * 4, ld * 4},
                     {"workspace", workspace, 1, (int64_t)w.total, (int64_t)w.total},

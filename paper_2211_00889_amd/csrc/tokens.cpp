@@ -88,15 +88,12 @@ nbsgd_status check_embed(int32_t T, int32_t vocab, int32_t dim) {
   return NBSGD_OK;
 }
 
-EmbedSpace embed_space(int64_t groups, int64_t T, int64_t vocab, int64_t dim) {
+EmbedSpace embed_space(int64_t groups, int64_t T, int64_t dim) {
   EmbedSpace s;
-  s.merged = 2 * T > vocab;
-  const int64_t all = s.merged ? T + vocab : T;
-  // tokens alone: 32 of them (16 mini-batches of 8192 x 512: 264 us, 16 tokens 267, 64 tokens 272);
-  // merged, a piece has rows without tokens too, and takes 64 entries.  Fewer where a mini-batch
-  // is small and the time is a piece's own
-  s.items = all < 32 * 64 ? 16 : !s.merged || all < 64 * 64 ? 32 : kMaxPiece;
-  s.pieces = ceil_div(all, s.items);
+  // of 32 tokens (16 mini-batches of 8192 x 512: 264 us, 16 tokens 267, 64 tokens 272); of 16
+  // where a mini-batch has few and the time is a piece's own
+  s.items = T < 64 * kMaxPiece ? 16 : kMaxPiece;
+  s.pieces = ceil_div(T, s.items);
   s.keys = 0;
   s.sorted = s.keys + up256((size_t)groups * T * 8);
   s.flags = s.sorted + up256((size_t)groups * T * 8);
@@ -160,7 +157,7 @@ extern "C" nbsgd_status nbsgd_embed_workspace_bytes(int32_t n, int32_t m, int32_
   if (nbsgd_status st = check_nm(n, m)) return st;
   if (nbsgd_status st = check_embed(T, vocab, dim)) return st;
   if (!bytes) return fail(NBSGD_E_ARG, "bytes is null");
-  *bytes = embed_space((int64_t)n * m, T, vocab, dim).total;
+  *bytes = embed_space((int64_t)n * m, T, dim).total;
   return NBSGD_OK;
 }
 

@@ -56,16 +56,14 @@ nbsgd_status check_workspace(const void* ws, size_t bytes, size_t need);
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// ---- embeddings: pieces of the gradient's work (embed.hip), cut from a mini-batch's sorted tokens
-// merged with the table's rows, or from the tokens alone
-constexpr int kMaxPiece = 64;
+// ---- embeddings: pieces of a mini-batch's sorted tokens (embed.hip)
+constexpr int kMaxPiece = 32;
 struct EmbedSpace {
-  bool merged;
   int32_t items;      // of a piece
   int64_t pieces;     // of one mini-batch
   size_t keys, sorted, flags, parts, total;  // byte offsets, and the whole
 };
-EmbedSpace embed_space(int64_t groups, int64_t T, int64_t vocab, int64_t dim);
+EmbedSpace embed_space(int64_t groups, int64_t T, int64_t dim);
 nbsgd_status check_embed(int32_t T, int32_t vocab, int32_t dim);
 
 // ---- recurrence: tiles of NBSGD_SCAN_INTERVAL tokens
