@@ -485,7 +485,7 @@ nbsgd_status nbsgd_embed_grad(const void *dY, int64_t ldy, int32_t dtype, int32_
  * x, g     [n][m][batch][T] rows of dim elements, both ldx >= dim apart (they
  *          may be the two halves of one buffer's rows)
  * bias     device fp32 [dim] at bias + i*ld for learner i, or NULL (zero; ld
- *          is ignored)
+ *          is ignored); -inf counts as the lowest finite value
  * lengths  [n][m][batch], or NULL: every sequence has T tokens.  Values are
  *          clamped into [0, T].  Past its length a sequence's x and g are not
  *          read, h is 0 and the state stays as it is.

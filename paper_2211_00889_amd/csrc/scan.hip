@@ -104,15 +104,16 @@ __device__ __forceinline__ T* row_at(T* base, uint32_t bytes) {
   return reinterpret_cast<T*>(reinterpret_cast<char*>(base) + bytes);
 }
 
-// The lane's V biases.  -inf becomes the largest finite value (a is 0 all the same), so that
-// the gate of a token past the length, whose g is taken as the largest finite one, stays 1.
+// A channel's bias.  -inf becomes the lowest finite value (a is 0 all the same), so that the gate
+// of a token past the length, whose g is taken as +inf, is 1 with every bias.
+__device__ __forceinline__ float bias_at(const Call& c, int id, int ch) {
+  const float b = c.bias && ch < c.dim ? c.bias[(int64_t)(id / c.groups.m) * c.ld + ch] : 0.f;
+  return b == -__builtin_inff() ? -3.40282347e38f : b;
+}
 template <int V>
 __device__ __forceinline__ void load_bias(const Call& c, const Where& w, int ch, float (&bias)[V]) {
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    bias[v] = c.bias && ch + v < c.dim ? c.bias[(int64_t)(w.id / c.groups.m) * c.ld + ch + v] : 0.f;
-    if (bias[v] == -__builtin_inff()) bias[v] = -3e38f;
-  }
+  for (int v = 0; v < V; ++v) bias[v] = bias_at(c, w.id, ch + v);
 }
 
 __device__ __forceinline__ void expand(u32x2 r, float (&v)[4]) {
@@ -139,12 +140,12 @@ struct Word;
 template <>
 struct Word<float> {
   typedef uint32_t bits;
-  static constexpr uint32_t kPast = 0x7f7fffffu;  // the largest finite values
+  static constexpr uint32_t kPast = 0x7f800000u;  // infinities
 };
 template <>
 struct Word<__bf16> {
   typedef uint16_t bits;
-  static constexpr uint32_t kPast = 0x7f7f7f7fu;
+  static constexpr uint32_t kPast = 0x7f807f80u;
 };
 
 // The K rows from `base`, `ld` elements apart, of a lane `off` bytes into them: the first
@@ -660,7 +661,7 @@ __global__ void __launch_bounds__(256)
   if (ch >= c.dim) return;
   const int id = group_id(c.groups, e / c.batch);
   const int64_t seq = (int64_t)id * c.batch + e % c.batch;
-  const float bias = c.bias ? c.bias[(int64_t)(id / c.groups.m) * c.ld + ch] : 0.f;
+  const float bias = bias_at(c, id, ch);
   const int len = c.lengths ? min(max(c.lengths[seq], 0), c.T) : c.T;
   const T* x = static_cast<const T*>(c.x) + seq * c.T * c.ldx + ch;
   const T* g = static_cast<const T*>(c.g) + seq * c.T * c.ldx + ch;
@@ -686,7 +687,7 @@ __global__ void __launch_bounds__(256)
   if (ch >= c.dim) return;
   const int id = group_id(c.groups, e / c.batch);
   const int64_t seq = (int64_t)id * c.batch + e % c.batch;
-  const float bias = c.bias ? c.bias[(int64_t)(id / c.groups.m) * c.ld + ch] : 0.f;
+  const float bias = bias_at(c, id, ch);
   const int len = c.lengths ? min(max(c.lengths[seq], 0), c.T) : c.T;
   const int64_t row0 = seq * c.T * c.ldx + ch;
   const T *x = static_cast<const T*>(c.x) + row0, *g = static_cast<const T*>(c.g) + row0;

@@ -489,6 +489,29 @@ def test_infinite_bias_and_empty_sequences():
     assert last[0, 0, 1].tolist() == [3.0, 5.0, 3.0] and (h[0, 0, 1, 300:] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T", [9, 200, 600])
+def test_lowest_biases(T, dtype):
+    """Biases of the lowest finite values: the tokens before the length replace the state, the ones
+    behind it leave it alone, backward too."""
+    lowest = -3.4028234663852886e38
+    X = torch.tensor([[0.0, 0, 0, 0, lowest, -3.39e38, -3.2e38, -float("inf"), 0.0, 0, 0, 0]], device=DEV)
+    C, L = 4, T - 4
+    x, g = torch.full((1, 1, 1, T, C), 3.0, dtype=dtype, device=DEV), torch.zeros((1, 1, 1, T, C), dtype=dtype, device=DEV)
+    h0 = torch.full((1, 1, 1, C), 5.0, device=DEV)
+    h, last = torch.empty_like(x), torch.empty_like(h0)
+    st = torch.empty((1, 1, 1, -(-T // nb.SCAN_INTERVAL), C), device=DEV)
+    lengths = torch.tensor([[[L]]], dtype=torch.int32, device=DEV)
+    ws = _ws(nb.scan_workspace_bytes(1, 1, 1, T, C))
+    nb.scan(x, g, [[1]], h, X=X, offset=4, h0=h0, h_last=last, lengths=lengths, states=st, workspace=ws)
+    assert (last == 3).all() and (h[0, 0, 0, :L] == 3).all() and (h[0, 0, 0, L:] == 0).all()
+    dx, dg, dl = torch.empty_like(x), torch.empty_like(x), torch.full_like(h0, 2.0)
+    nb.scan_grad(x, g, st, torch.ones_like(x), [[1]], dx, dg, ws, X=X, offset=4, dh_last=dl, dh0=last, lengths=lengths)
+    want = torch.ones(T, device=DEV)
+    want[L - 1], want[L:] = 3, 0
+    assert (dx[0, 0, 0].float() == want[:, None]).all() and (dg == 0).all() and (last == 0).all()
+
+
 # ------------------------------------------------------------- all of them
 def _one_pass(d, mask, sel=None):
     """Every call on the mini-batches of `mask`; the outputs by name.  `sel`: only mini-batch
