@@ -239,8 +239,8 @@ __device__ __forceinline__ void from_lds(const float* p, float (&v)[V]) {
 // split over workgroups.
 template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(64 * kScanWaves, 2)
-    k_scan(Call c, const float* __restrict__ h0, const float* __restrict__ carry,
-           T* __restrict__ h, int64_t ldh, float* __restrict__ h_last,
+    k_scan(Call c, const float* h0, const float* __restrict__ carry, T* __restrict__ h, int64_t ldh,
+           float* h_last,
            float* __restrict__ states) {
   using L = Lanes<T>;
   constexpr int V = L::V, K = L::K, CH = L::CH;
@@ -348,7 +348,10 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       if (n > 0 && (full || t + k < c.T)) store_row<T, WHOLE>(row_at(to + k * ldh, ih), r, n);
     }
   }
-  if (h_last && tile1 == c.tiles && keeper) h_last[w.seq * c.dim + own] = s;
+  if (h_last && tile1 == c.tiles) {  // uniform
+    __syncthreads();  // h_last may be h0, which every wave has read by now
+    if (keeper) h_last[w.seq * c.dim + own] = s;
+  }
 }
 
 // Composition of every tile of a split sequence, to `pairs`: of h -> a h + (1 - a) x (p is x), or,
@@ -466,9 +469,8 @@ __global__ void __launch_bounds__(512)
 template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(64 * kScanWaves, 2)
     k_scan_grad(Call c, const float* __restrict__ states, const T* __restrict__ dh, int64_t lddh,
-                const float* __restrict__ dh_last, const float* __restrict__ carry,
-                T* __restrict__ dx, T* __restrict__ dg,
-                float* __restrict__ dh0, float* __restrict__ part) {
+                const float* dh_last, const float* __restrict__ carry, T* __restrict__ dx,
+                T* __restrict__ dg, float* dh0, float* __restrict__ part) {
   using L = Lanes<T>;
   constexpr int V = L::V, K = L::K, CH = L::CH;
   __shared__ __attribute__((aligned(16))) float tot[2][4][kScanWaves][CH];
@@ -517,7 +519,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     const bool full = (tile + 1) * kScanTile <= w.len;
     T *tx = dx0 + (int64_t)(tile * kScanTile + 32 * wave) * c.ldx;
     T *tg = dg0 + (int64_t)(tile * kScanTile + 32 * wave) * c.ldx;
-    float* sums = part + ((w.seq * c.tiles + tile) * waves + wave) * c.dim + w.col + o;
+    const int64_t sums = ((w.seq * c.tiles + tile) * waves + wave) * c.dim + w.col + o;
     if (tile * kScanTile >= w.len) {  // uniform: behind the sequence
 #pragma unroll
       for (int k = 0; k < K; ++k)
@@ -528,7 +530,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       if (part && sub == 0)
 #pragma unroll
         for (int v = 0; v < V; ++v)
-          if (v < n) sums[v] = 0.f;
+          if (v < n) part[sums + v] = 0.f;
       if (tile > tile0) load_tile(tile - 1);
       continue;
     }
@@ -642,11 +644,14 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       if (sub == 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v)
-          if (v < n) sums[v] = sum[v];
+          if (v < n) part[sums + v] = sum[v];
       }
     }
   }
-  if (dh0 && tile0 == 0 && keeper) dh0[w.seq * c.dim + own] = mu;
+  if (dh0 && tile0 == 0) {  // uniform
+    __syncthreads();  // dh0 may be dh_last, which every wave has read by now
+    if (keeper) dh0[w.seq * c.dim + own] = mu;
+  }
 }
 
 // Sequences of at most kShort tokens (a served step above all), a channel a thread: the tile
@@ -654,8 +659,8 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
 constexpr int kShort = 16;
 template <typename T>
 __global__ void __launch_bounds__(256)
-    k_scan_short(Call c, const float* __restrict__ h0, T* __restrict__ h, int64_t ldh,
-                 float* __restrict__ h_last, float* __restrict__ states) {
+    k_scan_short(Call c, const float* h0, T* __restrict__ h, int64_t ldh, float* h_last,
+                 float* __restrict__ states) {
   const int cols = (c.dim + 255) / 256, e = blockIdx.x / cols;
   const int ch = blockIdx.x % cols * 256 + threadIdx.x;
   if (ch >= c.dim) return;
@@ -680,8 +685,8 @@ __global__ void __launch_bounds__(256)
 template <typename T>
 __global__ void __launch_bounds__(256)
     k_scan_grad_short(Call c, const float* __restrict__ states, const T* __restrict__ dh,
-                      int64_t lddh, const float* __restrict__ dh_last, T* __restrict__ dx,
-                      T* __restrict__ dg, float* __restrict__ dh0, float* __restrict__ part) {
+                      int64_t lddh, const float* dh_last, T* __restrict__ dx, T* __restrict__ dg,
+                      float* dh0, float* __restrict__ part) {
   const int cols = (c.dim + 255) / 256, e = blockIdx.x / cols;
   const int ch = blockIdx.x % cols * 256 + threadIdx.x;
   if (ch >= c.dim) return;
