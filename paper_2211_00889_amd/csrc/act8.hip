@@ -278,19 +278,19 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
   }
   const uint32_t aup = (uint32_t)(g >> 1) * (uint32_t)c.dim * kActBlock;  // to the lane's block of two
   const int four = tid / Q, q8 = tid % Q;  // the cell of B that this thread turns
-  // cells past the last column turn the tile's first ones, and a cell at the border whatever
-  // follows its row: nothing stores what they give
+  // cells past the last column turn the tile's first ones, and a cell at the border up to seven
+  // elements of whatever follows its row: nothing stores what they give
   const uint32_t boff = 2u * (uint32_t)(4 * four * (int)c.ldy + (8 * q8 < c.cols - c0 ? 8 * q8 : 0));
 
   u32x4 qa[MT], rb[4];
   uint32_t sa[MT];
   constexpr int kLoads = 2 * MT + 4;
-  // Whether a stage is read without looking: all its tokens are there, and whatever follows its
-  // rows (uniform).  What is no such stage reads the first packed bytes here, for nobody, so that
-  // the loads need no branch.
+  // Whether a stage is read without looking: all its tokens are there, and seven elements behind
+  // the last one's row (uniform).  What is no such stage reads the first packed bytes here, for
+  // nobody, so that the loads need no branch.
   auto plain = [&](int st) {
     const int end = (blk0 + kHB * (st + 1)) * kActBlock;
-    return end <= tokens && (c0 + BN <= c.cols || end < c.T || id + 1 < c.batches);
+    return end <= tokens && (c0 + BN <= c.cols || (c.T - end) * c.ldy >= 7 || id + 1 < c.batches);
   };
   auto load_one = [&](int st, bool go, int k) {
     const int b = blk0 + kHB * st;

@@ -383,6 +383,26 @@ def test_act_grad(n, m, T, dim, out, gap, shift):
     assert (G[:, :, :offset] == SENTINEL).all() and (G[:, :, offset + dim * out:] == SENTINEL).all()
 
 
+@pytest.mark.parametrize("out", [1, 2, 3, 5, 6, 7, 9])
+@pytest.mark.parametrize("T", [64, 65, 67, 71, 128, 131])
+def test_act_grad_narrow_rows(T, out):
+    """Rows shorter than the 16 bytes of a load, whose last ones end with the buffer; what stands
+    behind them, NaNs here, is in no result."""
+    rng = np.random.default_rng(T + out)
+    _say(f"act_grad T={T} out={out}")
+    dim = 20
+    A, _ = _rows((1, 1, T, dim), BF16, rng=rng)
+    dY, whole = _rows((1, 1, T, out), BF16, rng=rng)
+    whole[T * out:] = float("nan")
+    packed = torch.zeros((1, 1, nb.act_bytes(T, dim)), dtype=torch.uint8, device=DEV)
+    nb.act_pack(A, [[1]], packed)
+    G = torch.empty((1, 1, dim * out), device=DEV)
+    nb.act_grad(packed, dY, [[1]], G, 0, dim)
+    q, step = orc.act8(_np(A[0, 0]))
+    want, bound = orc.act_grad(q * step, _np(dY[0, 0]))
+    _close("G", G[0, 0].view(dim, out), want, bound)
+
+
 # ---------------------------------------------- far rows, states in place
 def test_rows_beyond_32_bits():
     """Rows so far apart that byte offsets pass 2^32, and a table of more than 2^31 floats."""
