@@ -2,6 +2,7 @@
 // them (gfx950).  Packed layout of a mini-batch: block of 32 tokens, channel, 32 int8; then
 // group of four blocks, channel, four step exponents (k + 127; 255 for NaNs).
 #include <algorithm>
+#include <type_traits>
 
 #include "device_rows.h"
 
@@ -223,7 +224,7 @@ struct GradCall {
   int64_t ldy, ld;  // of out: floats from one mini-batch to the next
   int64_t part;     // floats from one part to the next
   int32_t T, dim, cols, parts, per;  // per: blocks of a part, a multiple of four
-  int32_t batches;                   // mini-batches of dY
+  int32_t batches, border;           // mini-batches of dY; tokens that seven elements follow
   int32_t tm, tn, items;
   Act8 lay;
   Groups groups;
@@ -285,26 +286,20 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
   u32x4 qa[MT], rb[4];
   uint32_t sa[MT];
   constexpr int kLoads = 2 * MT + 4;
-  // Whether a stage is read without looking: all its tokens are there, and seven elements behind
-  // the last one's row (uniform).  What is no such stage reads the first packed bytes here, for
-  // nobody, so that the loads need no branch.
-  auto plain = [&](int st) {
-    const int end = (blk0 + kHB * (st + 1)) * kActBlock;
-    return end <= tokens && (c0 + BN <= c.cols || (c.T - end) * c.ldy >= 7 || id + 1 < c.batches);
-  };
-  auto load_one = [&](int st, bool go, int k) {
+  // The first stages are read without looking: all their tokens are there, and seven elements
+  // behind the last one's row
+  const int sure = c0 + BN <= c.cols || id + 1 < c.batches ? tokens : min(tokens, c.border);
+  const int plain = max(0, sure / kActBlock - blk0) / kHB;
+  auto load_one = [&](int st, int k) {
     const int b = blk0 + kHB * st;
-    const uint32_t on = go ? ~0u : 0u;
-    if (k < 4) {
-      const uint8_t* from = go ? reinterpret_cast<const uint8_t*>(rows + (int64_t)(b * kActBlock + k) * c.ldy) : base;
-      rb[k] = *reinterpret_cast<const u32x4_any*>(from + (boff & on));
-    } else if (k < 4 + MT) {
-      const uint8_t* from = base + (go ? (int64_t)b * c.dim * kActBlock : 0);
-      qa[k - 4] = *reinterpret_cast<const u32x4*>(from + ((aoff[k - 4] + aup) & on));
-    } else {
-      const uint8_t* from = base + (go ? c.lay.scale + (int64_t)(b >> 2) * c.dim * 4 : 0);
-      sa[k - 4 - MT] = *reinterpret_cast<const uint32_t*>(from + (soff[k - 4 - MT] & on));
-    }
+    if (k < 4)
+      rb[k] = *reinterpret_cast<const u32x4_any*>(
+          reinterpret_cast<const uint8_t*>(rows + (int64_t)(b * kActBlock + k) * c.ldy) + boff);
+    else if (k < 4 + MT)
+      qa[k - 4] = *reinterpret_cast<const u32x4*>(base + (int64_t)b * c.dim * kActBlock + (aoff[k - 4] + aup));
+    else
+      sa[k - 4 - MT] = *reinterpret_cast<const uint32_t*>(base + c.lay.scale + (int64_t)(b >> 2) * c.dim * 4 +
+                                                          soff[k - 4 - MT]);
   };
   // Any stage: blocks past the last are read as it, tokens and columns past the last as zeros
   auto load_any = [&](int st) {
@@ -350,8 +345,9 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
     const int h = n / F, f = wn * F + n % F;
     return *reinterpret_cast<const bf16x8*>(&Bs[buf][2 * g + h][f % 8 * Q + 16 * (f / 8) + i][0]);
   };
-  // A stage's products, RING fragments read ahead, with the next stage's loads among them
-  auto multiply = [&](int buf, int next, bool go) {
+  // A stage's products, RING fragments read ahead, with the next stage's loads among them or not
+  auto multiply = [&](int buf, int next, auto loads) {
+    constexpr int kAmong = decltype(loads)::value ? kLoads : 0;
     // the products first: the two waves of a SIMD would otherwise stage and multiply in step
     __builtin_amdgcn_s_setprio(1);
     bf16x8 B[RING];
@@ -363,14 +359,14 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
       for (int a = 0; a < MT; ++a)
         acc[a][n % F] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[n / F][a], B[n % RING], acc[a][n % F], 0, 0, 0);
       if (n + RING < STEPS) B[n % RING] = read_b(buf, n + RING);
-      if (n < kLoads) load_one(next, go, n);
+      if (n < kAmong) load_one(next, n);
     }
     __builtin_amdgcn_sched_group_barrier(0x100, RING, 0);  // LDS reads
 #pragma unroll
     for (int n = 0; n < STEPS; ++n) {
       __builtin_amdgcn_sched_group_barrier(0x008, MT, 0);  // MFMAs
       if (n + RING < STEPS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      if (n < kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // load
+      if (n < kAmong) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // load
     }
     __builtin_amdgcn_s_setprio(0);
   };
@@ -381,16 +377,20 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
     make_a(0);
   }
   __syncthreads();
-  for (int st = 0; st < stages; ++st) {
-    const int buf = st & 1;
-    const bool go = plain(st + 1);
-    multiply(buf, st + 1, go);
-    if (st + 1 < stages && !go) load_any(st + 1);
-    if (st + 1 < stages) {
-      stage(buf ^ 1);
-      make_a(st + 1);
-      __syncthreads();
-    }
+  int st = 0;
+  for (; st + 1 < plain; ++st) {
+    multiply(st & 1, st + 1, std::true_type());
+    stage(~st & 1);
+    make_a(st + 1);
+    __syncthreads();
+  }
+  for (; st < stages; ++st) {
+    multiply(st & 1, 0, std::false_type());
+    if (st + 1 == stages) break;
+    load_any(st + 1);
+    stage(~st & 1);
+    make_a(st + 1);
+    __syncthreads();
   }
   float* out = c.out + id * c.ld + part * c.part;
 #pragma unroll
@@ -543,6 +543,7 @@ extern "C" nbsgd_status nbsgd_act_grad(const void* packed, const void* dY, int64
   c.dim = dim;
   c.cols = out;
   c.batches = n * m;
+  c.border = T - (int32_t)ceil_div(7, ldy);
   c.parts = act8_splits(T, dim, out);
   c.per = (int32_t)(ceil_div(ceil_div(lay.blocks, c.parts), 4) * 4);
   c.lay = lay;
