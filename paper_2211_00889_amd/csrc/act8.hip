@@ -2,7 +2,6 @@
 // them (gfx950).  Packed layout of a mini-batch: block of 32 tokens, channel, 32 int8; then
 // group of four blocks, channel, four step exponents (k + 127; 255 for NaNs).
 #include <algorithm>
-#include <type_traits>
 
 #include "device_rows.h"
 
@@ -285,21 +284,22 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
 
   u32x4 qa[MT], rb[4];
   uint32_t sa[MT];
-  constexpr int kLoads = 2 * MT + 4;
-  // The first stages are read without looking: all their tokens are there, and seven elements
+  // The first `plain` stages are read without looking: all their tokens are there, and seven elements
   // behind the last one's row
   const int sure = c0 + BN <= c.cols || id + 1 < c.batches ? tokens : min(tokens, c.border);
   const int plain = max(0, sure / kActBlock - blk0) / kHB;
-  auto load_one = [&](int st, int k) {
-    const int b = blk0 + kHB * st;
-    if (k < 4)
-      rb[k] = *reinterpret_cast<const u32x4_any*>(
-          reinterpret_cast<const uint8_t*>(rows + (int64_t)(b * kActBlock + k) * c.ldy) + boff);
-    else if (k < 4 + MT)
-      qa[k - 4] = *reinterpret_cast<const u32x4*>(base + (int64_t)b * c.dim * kActBlock + (aoff[k - 4] + aup));
-    else
-      sa[k - 4 - MT] = *reinterpret_cast<const uint32_t*>(base + c.lay.scale + (int64_t)(b >> 2) * c.dim * 4 +
-                                                          soff[k - 4 - MT]);
+  auto load_rows = [&](int st) {
+    const uint8_t* from = reinterpret_cast<const uint8_t*>(rows + (int64_t)(blk0 + kHB * st) * kActBlock * c.ldy);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) rb[t] = *reinterpret_cast<const u32x4_any*>(from + 2 * t * c.ldy + boff);
+  };
+  auto load_packed = [&](int st) {
+    const int64_t b = blk0 + kHB * st;
+#pragma unroll
+    for (int a = 0; a < MT; ++a) {
+      qa[a] = *reinterpret_cast<const u32x4*>(base + b * c.dim * kActBlock + (aoff[a] + aup));
+      sa[a] = *reinterpret_cast<const uint32_t*>(base + c.lay.scale + (b >> 2) * c.dim * 4 + soff[a]);
+    }
   };
   // Any stage: blocks past the last are read as it, tokens and columns past the last as zeros
   auto load_any = [&](int st) {
@@ -316,6 +316,14 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
       const int tok = b * kActBlock + 4 * four + t;
       rb[t] = (u32x4){0u, 0u, 0u, 0u};
       if (tok < tokens && n > 0) rb[t] = load16<__bf16>(rows + (int64_t)tok * c.ldy + 8 * q8, n);
+    }
+  };
+  auto load = [&](int st) {
+    if (st < plain) {
+      load_rows(st);
+      load_packed(st);
+    } else if (st < stages) {
+      load_any(st);
     }
   };
   auto stage = [&](int buf) {
@@ -345,9 +353,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
     const int h = n / F, f = wn * F + n % F;
     return *reinterpret_cast<const bf16x8*>(&Bs[buf][2 * g + h][f % 8 * Q + 16 * (f / 8) + i][0]);
   };
-  // A stage's products, RING fragments read ahead, with the next stage's loads among them or not
-  auto multiply = [&](int buf, int next, auto loads) {
-    constexpr int kAmong = decltype(loads)::value ? kLoads : 0;
+  // A stage's products, RING fragments read ahead
+  auto multiply = [&](int buf) {
     // the products first: the two waves of a SIMD would otherwise stage and multiply in step
     __builtin_amdgcn_s_setprio(1);
     bf16x8 B[RING];
@@ -359,37 +366,38 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
       for (int a = 0; a < MT; ++a)
         acc[a][n % F] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[n / F][a], B[n % RING], acc[a][n % F], 0, 0, 0);
       if (n + RING < STEPS) B[n % RING] = read_b(buf, n + RING);
-      if (n < kAmong) load_one(next, n);
     }
     __builtin_amdgcn_sched_group_barrier(0x100, RING, 0);  // LDS reads
 #pragma unroll
     for (int n = 0; n < STEPS; ++n) {
       __builtin_amdgcn_sched_group_barrier(0x008, MT, 0);  // MFMAs
       if (n + RING < STEPS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      if (n < kAmong) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // load
     }
     __builtin_amdgcn_s_setprio(0);
   };
 
+  load(0);
   if (stages > 0) {
-    load_any(0);
     stage(0);
     make_a(0);
   }
+  load(1);
   __syncthreads();
   int st = 0;
-  for (; st + 1 < plain; ++st) {
-    multiply(st & 1, st + 1, std::true_type());
+  for (; st + 2 < plain; ++st) {
+    multiply(st & 1);
     stage(~st & 1);
+    load_rows(st + 2);
     make_a(st + 1);
+    load_packed(st + 2);
     __syncthreads();
   }
   for (; st < stages; ++st) {
-    multiply(st & 1, 0, std::false_type());
+    multiply(st & 1);
     if (st + 1 == stages) break;
-    load_any(st + 1);
     stage(~st & 1);
     make_a(st + 1);
+    load(st + 2);
     __syncthreads();
   }
   float* out = c.out + id * c.ld + part * c.part;
