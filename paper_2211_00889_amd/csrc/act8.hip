@@ -2,6 +2,7 @@
 // them (gfx950).  Packed layout of a mini-batch: block of 32 tokens, channel, 32 int8; then
 // group of four blocks, channel, four step exponents (k + 127; 255 for NaNs).
 #include <algorithm>
+#include <type_traits>
 
 #include "device_rows.h"
 
@@ -200,14 +201,16 @@ __global__ void __launch_bounds__(256)
 //      column to LDS, column 8 q + e of the tile to slot e * BN / 8 + q, so that the writes and
 //      the fragment reads are contiguous and a lane's results of eight (or four) fragments are
 //      consecutive columns.
-// A wave takes 16 MT channels x 16 F columns, WM x WN waves a tile.  Two buffers of B, one
-// barrier a stage.  The next stage's loads go out one by one among this stage's MFMAs.
-// 32 mini-batches of 4096 x 1024 x 2048: 545 us, 1.01 PFLOP/s (a library's bf16 product of
-// 8192^3 reaches 1.17).  What bounds it: the MFMAs are 240 us of it and the stage's other parts
-// hardly hide behind them, since a barrier a stage keeps the two waves of a SIMD in step; with
-// no loads it took 400, with no unpacking 508, without the turning 529.  128 tokens a
-// stage 542; 64 channels x 256 columns a wave 808, x 128 663; two workgroups of four such
-// waves a CU 583.
+// A wave takes 16 MT channels x 16 F columns, WM x WN waves a tile.  Two buffers of B; a stage's
+// loads go out a whole stage before they are wanted.  Of eight waves, two on each SIMD (waves w
+// and w + 4), the late half runs half a stage behind: while one wave of a SIMD multiplies, the
+// other one unpacks, turns and loads, and two barriers a stage keep it so.
+// 32 mini-batches of 4096 x 1024 x 2048: 482 us, 1.14 PFLOP/s (a library's bf16 product of
+// 8192^3 reaches 1.17); 514 us over many passes, against 526 with both halves in step.  What
+// bounds it is power: 0.93 million cycles at 1.9 GHz, 0.52 of them the MFMAs' own, where both
+// halves in step and loads among the products took 1.21 million at 2.2 GHz.  Of the 514 us no
+// loads save 94, half the MFMAs 63, no unpacking 56, no turning 32, no LDS reads 25.  128 tokens a
+// stage, 64 channels x 256 or 128 columns a wave, two workgroups of four waves a CU took longer.
 constexpr int kHB = 2, kStageTokens = kActBlock * kHB;
 template <int MT, int F, int WM, int WN>
 struct GradTile {
@@ -302,15 +305,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
     }
   };
   // Any stage: blocks past the last are read as it, tokens and columns past the last as zeros
-  auto load_any = [&](int st) {
-    const int b = blk0 + kHB * st;
-    const int blk = min(b + (g >> 1), blk1 - 1);
-#pragma unroll
-    for (int a = 0; a < MT; ++a) {
-      qa[a] = *reinterpret_cast<const u32x4*>(base + (int64_t)blk * c.dim * kActBlock + aoff[a]);
-      sa[a] = *reinterpret_cast<const uint32_t*>(base + c.lay.scale + (int64_t)(b >> 2) * c.dim * 4 + soff[a]);
-    }
-    const int n = c.cols - c0 - 8 * q8;
+  auto any_rows = [&](int st) {
+    const int b = blk0 + kHB * st, n = c.cols - c0 - 8 * q8;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int tok = b * kActBlock + 4 * four + t;
@@ -318,12 +314,13 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
       if (tok < tokens && n > 0) rb[t] = load16<__bf16>(rows + (int64_t)tok * c.ldy + 8 * q8, n);
     }
   };
-  auto load = [&](int st) {
-    if (st < plain) {
-      load_rows(st);
-      load_packed(st);
-    } else if (st < stages) {
-      load_any(st);
+  auto any_packed = [&](int st) {
+    const int b = blk0 + kHB * st;
+    const int blk = min(b + (g >> 1), blk1 - 1);
+#pragma unroll
+    for (int a = 0; a < MT; ++a) {
+      qa[a] = *reinterpret_cast<const u32x4*>(base + (int64_t)blk * c.dim * kActBlock + aoff[a]);
+      sa[a] = *reinterpret_cast<const uint32_t*>(base + c.lay.scale + (int64_t)(b >> 2) * c.dim * 4 + soff[a]);
     }
   };
   auto stage = [&](int buf) {
@@ -355,8 +352,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
   };
   // A stage's products, RING fragments read ahead
   auto multiply = [&](int buf) {
-    // the products first: the two waves of a SIMD would otherwise stage and multiply in step
-    __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_s_setprio(1);  // the products first
     bf16x8 B[RING];
 #pragma unroll
     for (int n = 0; n < RING; ++n) B[n] = read_b(buf, n);
@@ -376,50 +372,77 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
     __builtin_amdgcn_s_setprio(0);
   };
 
-  load(0);
-  if (stages > 0) {
-    stage(0);
-    make_a(0);
-  }
-  load(1);
-  __syncthreads();
-  int st = 0;
-  for (; st + 2 < plain; ++st) {
-    multiply(st & 1);
-    stage(~st & 1);
-    load_rows(st + 2);
-    make_a(st + 1);
-    load_packed(st + 2);
+  constexpr bool PAIR = WM * WN == 8;
+  auto meet = [&]() {  // nothing of one side moves to the other
+    __builtin_amdgcn_sched_barrier(0);
     __syncthreads();
-  }
-  for (; st < stages; ++st) {
-    multiply(st & 1);
-    if (st + 1 == stages) break;
-    stage(~st & 1);
-    make_a(st + 1);
-    load(st + 2);
-    __syncthreads();
-  }
-  float* out = c.out + id * c.ld + part * c.part;
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // The wave's way through the tile.  The first half multiplies stage st and then brings its part
+  // of stage st + 1's B to LDS; the late half brings that part and multiplies stage st then.  So
+  // B's buffer st + 1 is written after both halves' products of stage st - 1 and before theirs of
+  // st + 1, and both meet equally often.
+  auto walk = [&](auto half) {
+    constexpr bool late = decltype(half)::value;
+    if (stages > 0) {
+      any_rows(0);
+      any_packed(0);
+      stage(0);
+      if (!late) make_a(0);
+    }
+    if (stages > 1) {
+      any_rows(1);
+      if (!late) any_packed(1);
+    }
+    meet();
+    int st = 0;
+    for (; st + 2 < plain; ++st) {
+      if (!late) multiply(st & 1);
+      if (PAIR && !late) meet();
+      stage(~st & 1);
+      load_rows(st + 2);
+      make_a(st + 1 - late);
+      load_packed(st + 2 - late);
+      if (late) meet();
+      if (late) multiply(st & 1);
+      meet();
+    }
+    for (; st < stages; ++st) {
+      if (!late) multiply(st & 1);
+      if (PAIR && !late) meet();
+      if (st + 1 < stages) stage(~st & 1);
+      if (st + 2 < stages) any_rows(st + 2);
+      if (st + 1 - late < stages) make_a(st + 1 - late);
+      if (st + 2 - late < stages) any_packed(st + 2 - late);
+      if (late) meet();
+      if (late) multiply(st & 1);
+      meet();
+    }
+    float* out = c.out + id * c.ld + part * c.part;
 #pragma unroll
-  for (int a = 0; a < MT; ++a)
+    for (int a = 0; a < MT; ++a)
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int ch = k0 + 16 * a + 4 * g + t;
-      if (ch >= c.dim) continue;
+      for (int t = 0; t < 4; ++t) {
+        const int ch = k0 + 16 * a + 4 * g + t;
+        if (ch >= c.dim) continue;
 #pragma unroll
-      for (int f = 0; f < F; f += 4) {
-        const int e = (wn * F + f) % 8, col = c0 + 8 * (16 * ((wn * F + f) / 8) + i) + e;
-        float* p = out + (int64_t)ch * c.cols + col;
-        if (col + 4 <= c.cols) {
-          *reinterpret_cast<f32x4_any*>(p) = (f32x4){acc[a][f][t], acc[a][f + 1][t], acc[a][f + 2][t], acc[a][f + 3][t]};
-        } else {
+        for (int f = 0; f < F; f += 4) {
+          const int e = (wn * F + f) % 8, col = c0 + 8 * (16 * ((wn * F + f) / 8) + i) + e;
+          float* p = out + (int64_t)ch * c.cols + col;
+          if (col + 4 <= c.cols) {
+            *reinterpret_cast<f32x4_any*>(p) = (f32x4){acc[a][f][t], acc[a][f + 1][t], acc[a][f + 2][t], acc[a][f + 3][t]};
+          } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (col + k < c.cols) p[k] = acc[a][f + k][t];
+            for (int k = 0; k < 4; ++k)
+              if (col + k < c.cols) p[k] = acc[a][f + k][t];
+          }
         }
       }
-    }
+  };
+  if constexpr (PAIR) {
+    if (wave >= 4) return walk(std::true_type());
+  }
+  walk(std::false_type());
 }
 
 // The parts' sums in order.

@@ -383,6 +383,28 @@ def test_act_grad(n, m, T, dim, out, gap, shift):
     assert (G[:, :, :offset] == SENTINEL).all() and (G[:, :, offset + dim * out:] == SENTINEL).all()
 
 
+@pytest.mark.parametrize("T", [1, 63, 64, 65, 128, 129, 192, 193, 257, 321, 384, 500])
+@pytest.mark.parametrize("n,m,dim,out", [(16, 16, 33, 70), (16, 16, 270, 12), (8, 8, 130, 260), (2, 8, 500, 1030)])
+def test_act_grad_many(n, m, dim, out, T):
+    """So many mini-batches or columns that the larger tiles are taken, with every number of stages and
+    of tokens in the last one."""
+    rng = np.random.default_rng(T + dim)
+    _say(f"act_grad {n}x{m} T={T} dim={dim} out={out}")
+    A, _ = _rows((n, m, T, dim), BF16, rng=rng)
+    dY, _ = _rows((n, m, T, out), BF16, rng=rng)
+    packed = torch.empty((n, m, nb.act_bytes(T, dim)), dtype=torch.uint8, device=DEV)
+    mask = np.ones((n, m), np.uint8)
+    nb.act_pack(A, mask, packed)
+    values = torch.empty_like(A)
+    nb.act_unpack(packed, mask, values)
+    G = torch.full((n, m, (dim * out + 3) // 4 * 4), SENTINEL, device=DEV)
+    nb.act_grad(packed, dY, mask, G, 0, dim, _ws(nb.act_workspace_bytes(n, m, T, dim, out)))
+    for i in range(n):
+        for j in {0, m // 2, m - 1} if i in (0, n // 2, n - 1) else {(i * 5) % m}:
+            want, bound = orc.act_grad(_np(values[i, j]), _np(dY[i, j]))
+            _close("G", G[i, j, :dim * out].view(dim, out), want, bound)
+
+
 @pytest.mark.parametrize("out", [1, 2, 3, 5, 6, 7, 9])
 @pytest.mark.parametrize("T", [64, 65, 67, 71, 128, 131])
 def test_act_grad_narrow_rows(T, out):
