@@ -14,6 +14,7 @@
 // gradient mu_t = a_t (dh_t + mu_{t+1}) is the same kind of map from the last token to the
 // first; the states inside a tile are recomputed from the one kept at its start.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_rows.h"
 
@@ -148,16 +149,29 @@ struct Word<__bf16> {
   static constexpr uint32_t kPast = 0x7f807f80u;
 };
 
+// What the host has found of a call's rows:
+//   kOdd    not a whole number of a lane's 8 bytes
+//   kWhole  that
+//   kLines  and those that are written lie on whole 128-byte lines: stores past the caches.  128
+//           sequences of 1,024 x 1,024 bf16: 168 -> 163 us, backward 286 -> 277; with rows off the
+//           lines they lose what the caches put together (192 of 2,048 x 1,000: 495 -> 614 us)
+//   kFar    and those that are read, once and more than the memory-side cache keeps: loads past
+//           the caches too (163 -> 157, 277 -> 273; 128 of 512: 81 -> 93)
+enum Kind { kOdd, kWhole, kLines, kFar };
+
 // The K rows from `base`, `ld` elements apart, of a lane `off` bytes into them: the first
-// `live` are read (all of them in a FULL tile), the others are `past` in every word.  WHOLE:
-// rows are a whole number of 8 bytes; otherwise the lane's first n channels are read.
-template <typename T, bool WHOLE>
+// `live` are read (all of them in a FULL tile), the others are `past` in every word.  kOdd: the
+// lane's first n channels are read.
+template <typename T, Kind KIND>
 __device__ __forceinline__ void load_run(const T* base, int64_t ld, uint32_t off, bool full, int live,
                                          int n, uint32_t past, u32x2 (&r)[Lanes<T>::K]) {
   constexpr int K = Lanes<T>::K, V = Lanes<T>::V;
-  if (WHOLE && full) {  // uniform
+  if (KIND != kOdd && full) {  // uniform
 #pragma unroll
-    for (int k = 0; k < K; ++k) r[k] = *reinterpret_cast<const u32x2_any*>(row_at(base + k * ld, off));
+    for (int k = 0; k < K; ++k) {
+      const u32x2_any* p = reinterpret_cast<const u32x2_any*>(row_at(base + k * ld, off));
+      r[k] = KIND == kFar ? __builtin_nontemporal_load(p) : *p;
+    }
     return;
   }
 #pragma unroll
@@ -165,7 +179,7 @@ __device__ __forceinline__ void load_run(const T* base, int64_t ld, uint32_t off
     r[k] = (u32x2){past, past};
     if (k >= live) continue;
     const T* p = row_at(base + k * ld, off);
-    if (WHOLE || n >= V) {
+    if (KIND != kOdd || n >= V) {
       r[k] = *reinterpret_cast<const u32x2_any*>(p);
     } else {
       typedef typename Word<T>::bits bits;
@@ -178,10 +192,14 @@ __device__ __forceinline__ void load_run(const T* base, int64_t ld, uint32_t off
     }
   }
 }
-template <typename T, bool WHOLE>
+template <typename T, Kind KIND>
 __device__ __forceinline__ void store_row(T* p, u32x2 r, int n) {
   constexpr int V = Lanes<T>::V;
-  if (WHOLE || n >= V) {
+  if (KIND >= kLines) {
+    __builtin_nontemporal_store(r, reinterpret_cast<u32x2*>(p));
+    return;
+  }
+  if (KIND != kOdd || n >= V) {
     *reinterpret_cast<u32x2_any*>(p) = r;
     return;
   }
@@ -237,7 +255,7 @@ __device__ __forceinline__ void from_lds(const float* p, float (&v)[V]) {
 }
 // Forward, from h0, or from `carry` (the state at the start of every tile) where the sequence is
 // split over workgroups.
-template <typename T, bool WHOLE>
+template <typename T, Kind KIND>
 __global__ void __launch_bounds__(64 * kScanWaves, 2)
     k_scan(Call c, const float* h0, const float* __restrict__ carry, T* __restrict__ h, int64_t ldh,
            float* h_last,
@@ -279,8 +297,8 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     const int t = tile * kScanTile;
     const int64_t row = (int64_t)(t + 32 * wave) * c.ldx;
     const bool full = t + kScanTile <= w.len;
-    load_run<T, WHOLE>(x + row, c.ldx, ix, full, w.len - t - at, n, 0u, rx);
-    load_run<T, WHOLE>(g + row, c.ldx, ix, full, w.len - t - at, n, Word<T>::kPast, rg);
+    load_run<T, KIND>(x + row, c.ldx, ix, full, w.len - t - at, n, 0u, rx);
+    load_run<T, KIND>(g + row, c.ldx, ix, full, w.len - t - at, n, Word<T>::kPast, rg);
   };
   load_tile(tile0);
   for (int tile = tile0; tile < tile1; ++tile) {
@@ -291,7 +309,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       T* to = out0 + (int64_t)(tile * kScanTile + 32 * wave) * ldh;
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (n > 0 && t + k < c.T) store_row<T, WHOLE>(row_at(to + k * ldh, ih), (u32x2){0u, 0u}, n);
+        if (n > 0 && t + k < c.T) store_row<T, KIND>(row_at(to + k * ldh, ih), (u32x2){0u, 0u}, n);
       continue;
     }
     float a[K][V], b[K][V], A[V], B[V];
@@ -345,7 +363,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       for (int v = 0; v < V; ++v) hv[v] = fmaf(a[k][v], hv[v], b[k][v]);
       u32x2 r = collapse(hv);
       if (!full && t + k >= w.len) r = (u32x2){0u, 0u};
-      if (n > 0 && (full || t + k < c.T)) store_row<T, WHOLE>(row_at(to + k * ldh, ih), r, n);
+      if (n > 0 && (full || t + k < c.T)) store_row<T, KIND>(row_at(to + k * ldh, ih), r, n);
     }
   }
   if (h_last && tile1 == c.tiles) {  // uniform
@@ -357,7 +375,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
 // Composition of every tile of a split sequence, to `pairs`: of h -> a h + (1 - a) x (p is x), or,
 // REVERSE, of mu -> a (dh + mu) from a tile's last token to its first (p is dh).  As a rule a
 // tile a workgroup, and few enough registers for four of them a CU: what it waits for is its rows.
-template <typename T, bool REVERSE, bool WHOLE>
+template <typename T, bool REVERSE, Kind KIND>
 __global__ void __launch_bounds__(64 * kScanWaves, 8)
     k_scan_pairs(Call c, const T* __restrict__ p, int64_t ldp, float* __restrict__ pairs) {
   using L = Lanes<T>;
@@ -381,9 +399,9 @@ __global__ void __launch_bounds__(64 * kScanWaves, 8)
     const bool full = (tile + 1) * kScanTile <= w.len;
     const int live = w.len - tile * kScanTile - 32 * wave - sub * K;
     u32x2 rp[K], rg[K];
-    load_run<T, WHOLE>(p + row * ldp + w.col, ldp, (uint32_t)(sub * K * (int)ldp + (int)col) * (uint32_t)sizeof(T),
+    load_run<T, KIND>(p + row * ldp + w.col, ldp, (uint32_t)(sub * K * (int)ldp + (int)col) * (uint32_t)sizeof(T),
                        full, live, n, 0u, rp);
-    load_run<T, WHOLE>(static_cast<const T*>(c.g) + row * c.ldx + w.col, c.ldx,
+    load_run<T, KIND>(static_cast<const T*>(c.g) + row * c.ldx + w.col, c.ldx,
                        (uint32_t)(sub * K * (int)c.ldx + (int)col) * (uint32_t)sizeof(T), full, live, n,
                        Word<T>::kPast, rg);
     float A[V], B[V];
@@ -466,7 +484,7 @@ __global__ void __launch_bounds__(512)
 }
 
 // Backward, tiles from the last to the first; carry as in k_scan, for mu.
-template <typename T, bool WHOLE>
+template <typename T, Kind KIND>
 __global__ void __launch_bounds__(64 * kScanWaves, 2)
     k_scan_grad(Call c, const float* __restrict__ states, const T* __restrict__ dh, int64_t lddh,
                 const float* dh_last, const float* __restrict__ carry, T* __restrict__ dx,
@@ -508,10 +526,10 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     const int t = tile * kScanTile;
     const int64_t row = (int64_t)(t + 32 * wave) * c.ldx;
     const bool full = t + kScanTile <= w.len;
-    load_run<T, WHOLE>(x + row, c.ldx, ix, full, w.len - t - at, n, 0u, rx);
+    load_run<T, KIND>(x + row, c.ldx, ix, full, w.len - t - at, n, 0u, rx);
     s = own < c.dim ? states[(w.seq * c.tiles + tile) * c.dim + own] : 0.f;
-    load_run<T, WHOLE>(g + row, c.ldx, ix, full, w.len - t - at, n, Word<T>::kPast, rg);
-    load_run<T, WHOLE>(d + (int64_t)(t + 32 * wave) * lddh, lddh, id, full, w.len - t - at, n, 0u, rd);
+    load_run<T, KIND>(g + row, c.ldx, ix, full, w.len - t - at, n, Word<T>::kPast, rg);
+    load_run<T, KIND>(d + (int64_t)(t + 32 * wave) * lddh, lddh, id, full, w.len - t - at, n, 0u, rd);
   };
   load_tile(tile1 - 1);
   for (int tile = tile1 - 1; tile >= tile0; --tile) {
@@ -524,8 +542,8 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
 #pragma unroll
       for (int k = 0; k < K; ++k)
         if (n > 0 && t + k < c.T) {
-          store_row<T, WHOLE>(row_at(tx + k * c.ldx, ix), (u32x2){0u, 0u}, n);
-          store_row<T, WHOLE>(row_at(tg + k * c.ldx, ix), (u32x2){0u, 0u}, n);
+          store_row<T, KIND>(row_at(tx + k * c.ldx, ix), (u32x2){0u, 0u}, n);
+          store_row<T, KIND>(row_at(tg + k * c.ldx, ix), (u32x2){0u, 0u}, n);
         }
       if (part && sub == 0)
 #pragma unroll
@@ -632,8 +650,8 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
 #pragma unroll
       for (int v = 0; v < V; ++v) sum[v] += og[v];
       if (n > 0 && (full || t + k < c.T)) {
-        store_row<T, WHOLE>(row_at(tx + k * c.ldx, ix), collapse(ox), n);
-        store_row<T, WHOLE>(row_at(tg + k * c.ldx, ix), collapse(og), n);
+        store_row<T, KIND>(row_at(tx + k * c.ldx, ix), collapse(ox), n);
+        store_row<T, KIND>(row_at(tg + k * c.ldx, ix), collapse(og), n);
       }
     }
     if (part) {
@@ -805,7 +823,19 @@ nbsgd_status fill_call(Call* c, const void* x, const void* g, int64_t ldx, int32
   return check_groups(n, m, mask, &c->groups);
 }
 
-template <typename T, bool WHOLE>
+bool on_lines(const void* p, int64_t bytes) { return !((uintptr_t)p & 127) && bytes % 128 == 0; }
+
+// Calls f with the rows' kind as a constant.  `written` and `read`: whether those rows lie on
+// lines; `bytes`: what an unsplit call reads, against 1.5 times the memory-side cache.
+template <typename T, typename F>
+void by_kind(int dim, bool written, bool read, int64_t bytes, F f) {
+  if (dim % Lanes<T>::V) f(std::integral_constant<Kind, kOdd>());
+  else if (!written) f(std::integral_constant<Kind, kWhole>());
+  else if (!read || bytes < (int64_t)384 << 20) f(std::integral_constant<Kind, kLines>());
+  else f(std::integral_constant<Kind, kFar>());
+}
+
+template <typename T>
 nbsgd_status scan_forward(Call& c, const ScanSpace& w, const float* h0, void* h, int64_t ldh,
                           float* h_last, float* states, void* ws, hipStream_t s) {
   if (!c.groups.count) return NBSGD_OK;
@@ -820,22 +850,25 @@ nbsgd_status scan_forward(Call& c, const ScanSpace& w, const float* h0, void* h,
   c.chunk = d.chunk;
   c.items = (int32_t)(d.cols * d.seqs * d.chunks);
   const dim3 grid(8 * (unsigned)ceil_div(c.items, 8)), block(64 * d.waves);
-  float* carry = nullptr;
-  if (d.chunks > 1) {
-    float* pairs = reinterpret_cast<float*>(static_cast<char*>(ws) + w.pairs);
-    carry = reinterpret_cast<float*>(static_cast<char*>(ws) + w.carry);
-    Call each = c;
-    hipLaunchKernelGGL((k_scan_pairs<T, false, WHOLE>), tile_grid(&each, d), block, 0, s, each,
-                       static_cast<const T*>(c.x), c.ldx, pairs);
-    hipLaunchKernelGGL(k_scan_carry<false>, dim3((unsigned)(ceil_div(c.dim, 64) * d.seqs)), dim3(512), 0, s, c, pairs,
-                       h0, carry);
-  }
-  hipLaunchKernelGGL((k_scan<T, WHOLE>), grid, block, 0, s, c, h0, carry, out, ldh, h_last,
-                     states);
+  const bool split = d.chunks > 1;
+  float* pairs = reinterpret_cast<float*>(static_cast<char*>(ws) + w.pairs);
+  float* carry = split ? reinterpret_cast<float*>(static_cast<char*>(ws) + w.carry) : nullptr;
+  const int64_t e = sizeof(T), bytes = split ? 0 : 2 * seqs * c.T * c.dim * e;
+  by_kind<T>(c.dim, on_lines(h, ldh * e), on_lines(c.x, c.ldx * e) && on_lines(c.g, c.ldx * e), bytes, [&](auto kind) {
+    constexpr Kind KIND = decltype(kind)::value;
+    if (split) {
+      Call each = c;
+      hipLaunchKernelGGL((k_scan_pairs<T, false, std::min(KIND, kWhole)>), tile_grid(&each, d), block, 0, s, each,
+                         static_cast<const T*>(c.x), c.ldx, pairs);
+      hipLaunchKernelGGL(k_scan_carry<false>, dim3((unsigned)(ceil_div(c.dim, 64) * d.seqs)), dim3(512), 0, s, c,
+                         pairs, h0, carry);
+    }
+    hipLaunchKernelGGL((k_scan<T, KIND>), grid, block, 0, s, c, h0, carry, out, ldh, h_last, states);
+  });
   return launched("nbsgd_scan");
 }
 
-template <typename T, bool WHOLE>
+template <typename T>
 nbsgd_status scan_backward(Call& c, const ScanSpace& w, const float* states, const void* dh,
                            int64_t lddh, const float* dh_last, void* dx, void* dg, float* dh0,
                            float* Gbias, int64_t ld, void* ws, hipStream_t s) {
@@ -855,17 +888,24 @@ nbsgd_status scan_backward(Call& c, const ScanSpace& w, const float* states, con
     c.items = (int32_t)(d.cols * d.seqs * d.chunks);
     rows *= (int64_t)c.tiles * d.waves;
     const dim3 grid(8 * (unsigned)ceil_div(c.items, 8)), block(64 * d.waves);
-    float* carry = nullptr;
-    if (d.chunks > 1) {
-      float* pairs = reinterpret_cast<float*>(static_cast<char*>(ws) + w.pairs);
-      carry = reinterpret_cast<float*>(static_cast<char*>(ws) + w.carry);
-      Call each = c;
-      hipLaunchKernelGGL((k_scan_pairs<T, true, WHOLE>), tile_grid(&each, d), block, 0, s, each, d_in, lddh,
-                         pairs);
-      hipLaunchKernelGGL(k_scan_carry<true>, dim3((unsigned)(ceil_div(c.dim, 64) * d.seqs)), dim3(512), 0, s, c, pairs,
-                         dh_last, carry);
-    }
-    hipLaunchKernelGGL((k_scan_grad<T, WHOLE>), grid, block, 0, s, c, states, d_in, lddh, dh_last, carry, ox, og, dh0, part);
+    const bool split = d.chunks > 1;
+    float* pairs = reinterpret_cast<float*>(static_cast<char*>(ws) + w.pairs);
+    float* carry = split ? reinterpret_cast<float*>(static_cast<char*>(ws) + w.carry) : nullptr;
+    const int64_t e = sizeof(T), bytes = split ? 0 : 3 * seqs * c.T * c.dim * e;
+    const bool written = on_lines(dx, c.ldx * e) && on_lines(dg, c.ldx * e);
+    const bool read = on_lines(c.x, c.ldx * e) && on_lines(c.g, c.ldx * e) && on_lines(dh, lddh * e);
+    by_kind<T>(c.dim, written, read, bytes, [&](auto kind) {
+      constexpr Kind KIND = decltype(kind)::value;
+      if (split) {
+        Call each = c;
+        hipLaunchKernelGGL((k_scan_pairs<T, true, std::min(KIND, kWhole)>), tile_grid(&each, d), block, 0, s, each,
+                           d_in, lddh, pairs);
+        hipLaunchKernelGGL(k_scan_carry<true>, dim3((unsigned)(ceil_div(c.dim, 64) * d.seqs)), dim3(512), 0, s, c,
+                           pairs, dh_last, carry);
+      }
+      hipLaunchKernelGGL((k_scan_grad<T, KIND>), grid, block, 0, s, c, states, d_in, lddh, dh_last, carry, ox, og,
+                         dh0, part);
+    });
   }
   if (Gbias)
     hipLaunchKernelGGL(k_scan_bias, dim3((unsigned)ceil_div(c.dim, 64), c.groups.count), dim3(1024), 0,
@@ -912,8 +952,7 @@ extern "C" nbsgd_status nbsgd_scan(const void* x, const void* g, int64_t ldx, in
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   Call c;
   if (nbsgd_status st = fill_call(&c, x, g, ldx, n, m, batch, T, dim, bias, ld, lengths, mask)) return st;
-  const auto run = dtype == NBSGD_F32 ? (dim % 2 ? scan_forward<float, false> : scan_forward<float, true>)
-                                      : (dim % 4 ? scan_forward<__bf16, false> : scan_forward<__bf16, true>);
+  const auto run = dtype == NBSGD_F32 ? scan_forward<float> : scan_forward<__bf16>;
   return run(c, w, h0, h, ldh, h_last, states, workspace, s);
 }
 
@@ -962,7 +1001,6 @@ extern "C" nbsgd_status nbsgd_scan_grad(const void* x, const void* g, int64_t ld
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   Call c;
   if (nbsgd_status st = fill_call(&c, x, g, ldx, n, m, batch, T, dim, bias, ld, lengths, mask)) return st;
-  const auto run = dtype == NBSGD_F32 ? (dim % 2 ? scan_backward<float, false> : scan_backward<float, true>)
-                                      : (dim % 4 ? scan_backward<__bf16, false> : scan_backward<__bf16, true>);
+  const auto run = dtype == NBSGD_F32 ? scan_backward<float> : scan_backward<__bf16>;
   return run(c, w, states, dh, lddh, dh_last, dx, dg, dh0, Gbias, ld, workspace, s);
 }

@@ -295,6 +295,47 @@ def test_scan_token_by_token(dtype):
     assert torch.allclose(state, last, rtol=1e-5, atol=1e-5)
 
 
+@pytest.mark.parametrize("n,m,b,T,C,dtype", [
+    (1, 2, 3, 700, 64, BF16), (2, 1, 2, 300, 96, F32), (1, 1, 1, 1030, 128, BF16), (8, 8, 5, 40, 128, BF16),
+    (4, 8, 4, 700, 64, F32), (4, 8, 8, 520, 1024, BF16), (4, 8, 4, 530, 1024, F32),
+])
+def test_scan_rows_on_lines_and_off(n, m, b, T, C, dtype):
+    """Rows on whole 128-byte lines, few and many bytes of them, against the same rows 4 elements
+    further apart: bit for bit the same."""
+    _say(f"scan lines {n}x{m}x{b} T={T} dim={C} {dtype}")
+    gen = torch.Generator(device=DEV).manual_seed(T)
+    shape = (n, m, b, T, C)
+    x, g, dh = (torch.randn(shape, generator=gen, device=DEV).to(dtype) for _ in range(3))
+    h0, dl = (torch.randn((n, m, b, C), generator=gen, device=DEV) for _ in range(2))
+    X = torch.randn((n, C), generator=gen, device=DEV)
+    lengths = torch.randint(0, T + 1, (n, m, b), generator=gen, device=DEV, dtype=torch.int32)
+    mask, ws, results = np.ones((n, m), np.uint8), _ws(nb.scan_workspace_bytes(n, m, b, T, C)), []
+    for gap in (0, 4):
+        def rows(t=None):
+            view = torch.full((*shape[:-1], C + gap), SENTINEL, dtype=dtype, device=DEV)[..., :C]
+            return view if t is None else view.copy_(t)
+        px, pg, pd, h, dx, dg = rows(x), rows(g), rows(dh), rows(), rows(), rows()
+        last, st, d0 = torch.empty_like(h0), torch.empty((n, m, b, -(-T // nb.SCAN_INTERVAL), C), device=DEV), torch.empty_like(dl)
+        G = torch.empty((n, m, C), device=DEV)
+        nb.scan(px, pg, mask, h, X=X, h0=h0, h_last=last, lengths=lengths, states=st, workspace=ws)
+        nb.scan_grad(px, pg, st, pd, mask, dx, dg, ws, X=X, G=G, dh_last=dl, dh0=d0, lengths=lengths)
+        results.append([t.contiguous() for t in (h, last, st, dx, dg, d0, G)])
+        if gap:
+            assert all((torch.as_strided(t, (*shape[:-1], gap), t.stride(), t.storage_offset() + C) == SENTINEL).all()
+                       for t in (h, dx, dg))
+    assert all(torch.equal(p, q) for p, q in zip(*results))
+    i, j, k = n - 1, m - 1, b - 1  # one sequence's first channels against the oracle
+    L, few = int(lengths[i, j, k]), slice(0, 40)
+    args = [_np(t[i, j, k][..., few]) for t in (x, g)] + [_np(X[i, few]), _np(h0[i, j, k, few]), L]
+    (ho, _, s), (eh, _, es) = orc.scan(*args)
+    _close("h", results[0][0][i, j, k][:, few], ho, eh, dtype)
+    _close("h_last", results[0][1][i, j, k, few], s, es)
+    (gx, gg, g0, _), (ex, eg, e0, _) = orc.scan_grad(*args, _np(dh[i, j, k][..., few]), _np(dl[i, j, k, few]))
+    _close("dx", results[0][3][i, j, k][:, few], gx, ex, dtype)
+    _close("dg", results[0][4][i, j, k][:, few], gg, eg, dtype)
+    _close("dh0", results[0][5][i, j, k, few], g0, e0)
+
+
 # --------------------------------------------------------- 8-bit activations
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n,m,T,dim,gap,shift", [
