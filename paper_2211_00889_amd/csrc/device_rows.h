@@ -107,6 +107,9 @@ __device__ __forceinline__ void store16(T* p, u32x4 r, int n) {
     }
 }
 
+// Whether rows of `bytes` bytes apart lie on whole 128-byte lines.
+inline bool on_lines(const void* p, int64_t bytes) { return !((uintptr_t)p & 127) && bytes % 128 == 0; }
+
 // Refuses a stream of a device that is not the current one (kernels would be looked up on
 // the wrong one).
 inline nbsgd_status check_stream(void* stream) {

@@ -823,8 +823,6 @@ nbsgd_status fill_call(Call* c, const void* x, const void* g, int64_t ldx, int32
   return check_groups(n, m, mask, &c->groups);
 }
 
-bool on_lines(const void* p, int64_t bytes) { return !((uintptr_t)p & 127) && bytes % 128 == 0; }
-
 // Calls f with the rows' kind as a constant.  `written` and `read`: whether those rows lie on
 // lines; `bytes`: what an unsplit call reads, against 1.5 times the memory-side cache.
 template <typename T, typename F>

@@ -99,6 +99,34 @@ def test_embed(n, m, T, vocab, dim, gap, shift, offset, dtype):
     _gaps_untouched(Y, whole)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim,gap", [(64, 0), (64, 64), (192, 0), (520, 56), (1024, 0), (1000, 24)])
+def test_embed_rows_on_lines(dim, gap, dtype):
+    """Rows of whole 128-byte lines, with and without elements behind the last channel."""
+    n, m, T, vocab = 2, 2, 133, 90
+    rng = np.random.default_rng(dim)
+    X = torch.from_numpy(rng.normal(0, 1, (n, vocab * dim)).astype(np.float32)).to(DEV)
+    tok = rng.integers(-1, vocab + 1, (n, m, T)).astype(np.int32)
+    Y, whole = _rows((n, m, T, dim), dtype, gap)
+    nb.embed(X, 0, vocab, torch.from_numpy(tok).to(DEV), np.ones((n, m), np.uint8), Y, scale=0.5)
+    for i in range(n):
+        for j in range(m):
+            want = orc.embed(_np(X[i]).reshape(vocab, dim), tok[i, j], 0.5)
+            _close("Y", Y[i, j], want, orc.U * np.abs(want), dtype)
+    _gaps_untouched(Y, whole)
+    A = torch.full((n, m, T, dim), float("nan"), dtype=dtype, device=DEV)
+    packed = torch.empty((n, m, nb.act_bytes(T, dim)), dtype=torch.uint8, device=DEV)
+    nb.act_pack(Y, np.ones((n, m), np.uint8), packed)
+    nb.act_unpack(packed, np.ones((n, m), np.uint8), A)
+    back, whole = _rows((n, m, T, dim), dtype, gap + 1)
+    nb.act_unpack(packed, np.ones((n, m), np.uint8), back)
+    assert torch.equal(A, back)
+    line, whole = _rows((n, m, T, dim), dtype, gap)
+    nb.act_unpack(packed, np.ones((n, m), np.uint8), line)
+    assert torch.equal(A, line)
+    _gaps_untouched(line, whole)
+
+
 def _tokens(rng, kind, shape, vocab):
     if kind == "uniform":
         return rng.integers(-1, vocab + 1, shape).astype(np.int32)
