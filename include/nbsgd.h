@@ -481,7 +481,9 @@ nbsgd_status nbsgd_embed_grad(const void *dY, int64_t ldy, int32_t dtype, int32_
  * channel:
  *   a_t = 1 / (1 + exp(-(g_t + bias)))     h_t = a_t h_{t-1} + (1 - a_t) x_t
  * h_0 is the given first state or zero.  T = 1 with h0 and h_last is the form
- * that serves one token at a time; h_last may be h0 itself.
+ * that serves one token at a time; h_last may be h0 itself.  From a token whose
+ * x is infinite or NaN on, and with such an h_0, a channel's states are infinite
+ * or NaN, not always as the formula has them; the tokens before it are not.
  * x, g     [n][m][batch][T] rows of dim elements, both ldx >= dim apart (they
  *          may be the two halves of one buffer's rows)
  * bias     device fp32 [dim] at bias + i*ld for learner i, or NULL (zero; ld

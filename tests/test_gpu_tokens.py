@@ -728,6 +728,45 @@ def test_on_another_stream():
         assert torch.equal(o[k], want[k]), k
 
 
+def test_two_streams_at_once():
+    """Two callers with buffers of their own, taking turns at the launches."""
+    mask = np.ones((2, 3), np.uint8)
+    data = [_pass_inputs(seed, L=700) for seed in (8, 9)]
+    want = []
+    for d in data:
+        run, o = _one_pass(d, mask)
+        run()
+        want.append(o)
+    pairs = [_one_pass(d, mask) for d in data]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in data]
+    for _ in range(4):
+        for s, (run, _) in zip(streams, pairs):
+            with torch.cuda.stream(s):
+                run()
+    torch.cuda.synchronize()
+    for (_, o), w in zip(pairs, want):
+        for k in OUT:
+            assert torch.equal(o[k], w[k]), k
+
+
+@pytest.mark.parametrize("n,m,T,dim,out", [(16, 16, 200, 33, 72), (8, 8, 321, 130, 260), (2, 8, 2100, 500, 1032)])
+def test_act_grad_is_its_own_in_larger_tiles(n, m, T, dim, out):
+    """One of many mini-batches, whose call takes larger tiles, against the same one alone."""
+    rng = np.random.default_rng(T)
+    A, dY = (_rows((n, m, T, w), BF16, rng=rng)[0].contiguous() for w in (dim, out))
+    packed = torch.empty((n, m, nb.act_bytes(T, dim)), dtype=torch.uint8, device=DEV)
+    mask = np.ones((n, m), np.uint8)
+    nb.act_pack(A, mask, packed)
+    G = torch.empty((n, m, dim * out), device=DEV)
+    nb.act_grad(packed, dY, mask, G, 0, dim, _ws(nb.act_workspace_bytes(n, m, T, dim, out)))
+    for i, j in ((0, 0), (n - 1, m - 1), (n // 2, 1)):
+        one = torch.empty((1, 1, dim * out), device=DEV)
+        nb.act_grad(packed[i:i + 1, j:j + 1].contiguous(), dY[i:i + 1, j:j + 1].contiguous(), [[1]], one, 0, dim,
+                    _ws(nb.act_workspace_bytes(1, 1, T, dim, out)))
+        assert torch.equal(one[0, 0], G[i, j]), (i, j)
+
+
 def test_training_iteration():
     """Embeddings, a joint projection whose input is kept in 8 bits, the recurrence, a squared loss, and
     back: every gradient lands in its place of G and the fused step takes it.  Against the same model
