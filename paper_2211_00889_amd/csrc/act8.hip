@@ -496,7 +496,14 @@ nbsgd_status unpack_launch(const void* packed, int32_t Tn, int32_t dim, void* A,
   return launched("nbsgd_act_unpack");
 }
 
-constexpr int64_t kTileEnough = 256;
+// Which tile a call takes: the one whose tiles cost least.  A stage of a tile takes a full card
+// 8.6 ns (256 x 256), 3.2 (128 x 128) or 1.8 (64 x 128), 475 : 175 : 100, and a card with fewer
+// tiles than `least` is not full: one large tile a CU is, one middle or small one is not.
+//   1 mini-batch of 4096 x 2048 x 2048   large 91 us, middle 73, small 60
+//   8 of 4096 x 1024 x 1024              100, 95, 116
+//   64 of 512 x 512 x 512                29, 37, 38
+//   40 of 750 x 43 x 2225                55, 43, 29
+//   64 of 2048 x 256 x 256 in two parts  48, 45, 49
 constexpr int64_t kMaxStride = 1 << 22;  // 64 rows of dY lie within 32-bit offsets
 
 // Checks shared by the two directions.
@@ -593,11 +600,13 @@ extern "C" nbsgd_status nbsgd_act_grad(const void* packed, const void* dY, int64
   c.ld = c.parts > 1 ? c.parts * size : ld;
   c.part = size;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  // The largest tile that leaves no CU without one: its products per byte of LDS and of L2 are
-  // the most.
   const int64_t each = (int64_t)c.parts * g.count;
-  if (each * ceil_div(dim, 256) * ceil_div(out, 256) >= kTileEnough) grad_launch<2, 16, 8, 1>(c, s);
-  else if (each * ceil_div(dim, 128) * ceil_div(out, 128) >= kTileEnough) grad_launch<4, 4, 2, 2>(c, s);
+  const auto cost = [&](int64_t rows, int64_t columns, int64_t price, int64_t least) {
+    return price * std::max(each * ceil_div(dim, rows) * ceil_div(out, columns), least);
+  };
+  const int64_t large = cost(256, 256, 475, 256), middle = cost(128, 128, 175, 362), small = cost(64, 128, 100, 416);
+  if (large <= middle && large <= small) grad_launch<2, 16, 8, 1>(c, s);
+  else if (middle <= small) grad_launch<4, 4, 2, 2>(c, s);
   else grad_launch<2, 4, 2, 2>(c, s);
   if (c.parts > 1)
     hipLaunchKernelGGL(k_act8_parts, dim3((unsigned)std::min<int64_t>(ceil_div(size, 256), 1024), g.count),

@@ -453,7 +453,8 @@ def test_act_grad(n, m, T, dim, out, gap, shift):
 
 
 @pytest.mark.parametrize("T", [1, 63, 64, 65, 128, 129, 192, 193, 257, 321, 384, 500])
-@pytest.mark.parametrize("n,m,dim,out", [(16, 16, 33, 70), (16, 16, 270, 12), (8, 8, 130, 260), (2, 8, 500, 1030)])
+@pytest.mark.parametrize("n,m,dim,out", [(16, 16, 33, 70), (16, 16, 270, 12), (8, 8, 130, 260), (2, 8, 500, 1030),
+                                         (16, 16, 200, 250), (8, 16, 255, 497)])
 def test_act_grad_many(n, m, dim, out, T):
     """So many mini-batches or columns that the larger tiles are taken, with every number of stages and
     of tokens in the last one."""
@@ -750,7 +751,7 @@ def test_two_streams_at_once():
             assert torch.equal(o[k], w[k]), k
 
 
-@pytest.mark.parametrize("n,m,T,dim,out", [(16, 16, 200, 33, 72), (8, 8, 321, 130, 260), (2, 8, 2100, 500, 1032)])
+@pytest.mark.parametrize("n,m,T,dim,out", [(16, 16, 200, 200, 248), (8, 16, 321, 255, 500), (2, 8, 2100, 500, 1032)])
 def test_act_grad_is_its_own_in_larger_tiles(n, m, T, dim, out):
     """One of many mini-batches, whose call takes larger tiles, against the same one alone."""
     rng = np.random.default_rng(T)
