@@ -39,7 +39,7 @@ struct PackTile {
 
 // The V elements at p, the first n of them; zeros behind.
 __device__ __forceinline__ void load_v(const float* p, int n, float (&v)[4]) {
-  Elem<float>::expand(load16<float>(p, n), v);
+  Elem<float>::expand(load16(p, n), v);
 }
 __device__ __forceinline__ void load_v(const __bf16* p, int n, float (&v)[4]) {
   if (n >= 4) {
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
     for (int t = 0; t < 4; ++t) {
       const int tok = b * kActBlock + 4 * four + t;
       rb[t] = (u32x4){0u, 0u, 0u, 0u};
-      if (tok < tokens && n > 0) rb[t] = load16<__bf16>(rows + (int64_t)tok * c.ldy + 8 * q8, n);
+      if (tok < tokens && n > 0) rb[t] = load16(rows + (int64_t)tok * c.ldy + 8 * q8, n);
     }
   };
   auto any_packed = [&](int st) {

@@ -77,18 +77,26 @@ struct Elem<__bf16> {
   }
 };
 
-// The first `n` (at most V) elements at p as 16 bytes, zeros behind them.
-template <typename T>
-__device__ __forceinline__ u32x4 load16(const T* p, int n) {
-  constexpr int V = Elem<T>::V, per = V / 4;  // elements of a word
-  if (n >= V) return *reinterpret_cast<const u32x4_any*>(p);
+// The first `n` (at least one, V of them at most) elements at p as 16 bytes, zeros behind them.
+__device__ __forceinline__ u32x4 load16(const float* p, int n) {
+  if (n >= 4) return *reinterpret_cast<const u32x4_any*>(p);
   uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int k = 0; k < V; ++k)
-    if (k < n) {
-      if constexpr (per == 1) w[k] = __builtin_bit_cast(uint32_t, p[k]);
-      else w[k / per] |= (uint32_t)__builtin_bit_cast(uint16_t, p[k]) << (16 * (k % per));
-    }
+  for (int k = 0; k < 4; ++k)
+    if (k < n) w[k] = __builtin_bit_cast(uint32_t, p[k]);
+  return (u32x4){w[0], w[1], w[2], w[3]};
+}
+// The short ones read the last element over and over: behind branches the halves of a word
+// wait for each other.
+__device__ __forceinline__ u32x4 load16(const __bf16* p, int n) {
+  if (n >= 8) return *reinterpret_cast<const u32x4_any*>(p);
+  __bf16 v[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = p[min(k, n - 1)];
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    w[k / 2] |= k < n ? (uint32_t)__builtin_bit_cast(uint16_t, v[k]) << (16 * (k % 2)) : 0u;
   return (u32x4){w[0], w[1], w[2], w[3]};
 }
 template <typename T>

@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
     for (int q = 0; q < V / 4; ++q) {
       float w[4] = {0.f, 0.f, 0.f, 0.f};
-      if (inside && n > 4 * q) Elem<float>::expand(load16<float>(src + c + 4 * q, n - 4 * q), w);
+      if (inside && n > 4 * q) Elem<float>::expand(load16(src + c + 4 * q, n - 4 * q), w);
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[4 * q + k] = inside ? scale * w[k] : 0.f;
     }
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(256)
 
 // The first n (at most 4) elements at p, zeros behind them; and back.
 __device__ __forceinline__ void load4(const float* p, int n, float (&v)[4]) {
-  Elem<float>::expand(load16<float>(p, n), v);
+  Elem<float>::expand(load16(p, n), v);
 }
 __device__ __forceinline__ void load4(const __bf16* p, int n, float (&v)[4]) {
   if (n >= 4) {

@@ -154,46 +154,65 @@ struct Word<__bf16> {
 };
 
 // What the host has found of a call's rows:
-//   kOdd    not a whole number of a lane's 8 bytes
-//   kWhole  that
+//   kTiny   shorter than a lane's 8 bytes
+//   kOdd    not a whole number of them: a row's last lane reads the row's last 8 bytes and shifts
+//           (by elements its loads wait for each other: 48 sequences of 386 x 1527 bf16 77 -> 62
+//           us, backward 134 -> 103; 20 of 21265 x 19 126 -> 72, 187 -> 99)
+//   kWhole  a whole number
 //   kLines  and those that are written lie on whole 128-byte lines: stores past the caches.  128
 //           sequences of 1,024 x 1,024 bf16: 168 -> 163 us, backward 286 -> 277; with rows off the
 //           lines they lose what the caches put together (192 of 2,048 x 1,000: 495 -> 614 us)
 //   kFar    and those that are read, once and more than the memory-side cache keeps: loads past
 //           the caches too (163 -> 157, 277 -> 273; 128 of 512: 81 -> 93)
-enum Kind { kOdd, kWhole, kLines, kFar };
+enum Kind { kTiny, kOdd, kWhole, kLines, kFar };
 
+// Where a lane with n channels left from its first, `o` into the block, reads: `col` elements from
+// the base of the rows (taken kBack before the block's first channel), and the bits that it
+// shifts away.  Lanes past the last channel read the block's first ones, or the row's last.
+template <typename T, Kind KIND>
+struct Reads {
+  static constexpr int kBack = KIND == kOdd ? Lanes<T>::V : 0;
+  uint32_t col;
+  int shift, n;
+  __device__ __forceinline__ Reads(int o, int n_) : n(n_) {
+    const int skip = KIND == kOdd && n > 0 && n < Lanes<T>::V ? Lanes<T>::V - n : 0;
+    col = kBack + (n > 0 ? o - skip : KIND == kOdd ? o + n - Lanes<T>::V : 0);
+    shift = 8 * (int)sizeof(T) * skip;
+  }
+  // What is read as the lane's channels; where it is used, not where it is loaded, which would
+  // wait for it.
+  __device__ __forceinline__ u32x2 take(u32x2 r) const {
+    if constexpr (KIND == kOdd) return __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, r) >> shift);
+    return r;
+  }
+};
 // The K rows from `base`, `ld` elements apart, of a lane `off` bytes into them: the first
-// `live` are read (all of them in a FULL tile), the others are `past` in every word.  kOdd: the
-// lane's first n channels are read.
+// `live` are read (all of them in a FULL tile), the others are `past` in every word.
 template <typename T, Kind KIND>
 __device__ __forceinline__ void load_run(const T* base, int64_t ld, uint32_t off, bool full, int live,
-                                         int n, uint32_t past, u32x2 (&r)[Lanes<T>::K]) {
+                                         const Reads<T, KIND>& at, uint32_t past, u32x2 (&r)[Lanes<T>::K]) {
   constexpr int K = Lanes<T>::K, V = Lanes<T>::V;
-  if (KIND != kOdd && full) {  // uniform
+  auto load = [&](int k) -> u32x2 {
+    const T* p = row_at(base + k * ld, off);
+    const u32x2_any* q = reinterpret_cast<const u32x2_any*>(p);
+    if constexpr (KIND == kFar) return __builtin_nontemporal_load(q);
+    if constexpr (KIND != kTiny) return *q;
+    typedef typename Word<T>::bits bits;
+    uint32_t w[2] = {0u, 0u};
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const u32x2_any* p = reinterpret_cast<const u32x2_any*>(row_at(base + k * ld, off));
-      r[k] = KIND == kFar ? __builtin_nontemporal_load(p) : *p;
-    }
+    for (int v = 0; v < V; ++v)  // the last element over and over
+      w[v * sizeof(T) / 4] |= (uint32_t)__builtin_bit_cast(bits, p[max(min(v, at.n - 1), 0)]) << (8 * (v * sizeof(T) % 4));
+    return (u32x2){w[0], w[1]};
+  };
+  if (KIND != kTiny && full) {  // uniform
+#pragma unroll
+    for (int k = 0; k < K; ++k) r[k] = load(k);
     return;
   }
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     r[k] = (u32x2){past, past};
-    if (k >= live) continue;
-    const T* p = row_at(base + k * ld, off);
-    if (KIND != kOdd || n >= V) {
-      r[k] = *reinterpret_cast<const u32x2_any*>(p);
-    } else {
-      typedef typename Word<T>::bits bits;
-      uint32_t w[2] = {0u, 0u};
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (v < n)
-          w[v * sizeof(T) / 4] |= (uint32_t)__builtin_bit_cast(bits, p[v]) << (8 * (v * sizeof(T) % 4));
-      r[k] = (u32x2){w[0], w[1]};
-    }
+    if (k < live) r[k] = load(k);
   }
 }
 template <typename T, Kind KIND>
@@ -203,7 +222,7 @@ __device__ __forceinline__ void store_row(T* p, u32x2 r, int n) {
     __builtin_nontemporal_store(r, reinterpret_cast<u32x2*>(p));
     return;
   }
-  if (KIND != kOdd || n >= V) {
+  if (KIND >= kWhole || n >= V) {
     *reinterpret_cast<u32x2_any*>(p) = r;
     return;
   }
@@ -281,8 +300,9 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
   const int oc = lane & (CH - 1), own = w.col + oc;
   const bool keeper = wave == 0 && lane < CH && own < c.dim;
   const int64_t row0 = w.seq * c.T;
-  const T* x = static_cast<const T*>(c.x) + row0 * c.ldx + w.col;
-  const T* g = static_cast<const T*>(c.g) + row0 * c.ldx + w.col;
+  const Reads<T, KIND> in(o, n);
+  const T* x = static_cast<const T*>(c.x) + row0 * c.ldx + w.col - in.kBack;
+  const T* g = static_cast<const T*>(c.g) + row0 * c.ldx + w.col - in.kBack;
   T* out0 = h + row0 * ldh + w.col;
   float bias[V];
   load_bias<V>(c, w, w.col + o, bias);
@@ -293,16 +313,15 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     else if (h0) s = h0[w.seq * c.dim + own];
   }
   const int at = 32 * wave + sub * K;  // the lane's first token of a tile
-  const uint32_t col = n > 0 ? o : 0;  // lanes past the last channel read the first ones
-  const uint32_t ix = (uint32_t)(sub * K * (int)c.ldx + (int)col) * (uint32_t)sizeof(T);
+  const uint32_t ix = (uint32_t)(sub * K * (int)c.ldx + (int)in.col) * (uint32_t)sizeof(T);
   const uint32_t ih = (uint32_t)(sub * K * (int)ldh + o) * (uint32_t)sizeof(T);
   u32x2 rx[K], rg[K];
   auto load_tile = [&](int tile) {
     const int t = tile * kScanTile;
     const int64_t row = (int64_t)(t + 32 * wave) * c.ldx;
     const bool full = t + kScanTile <= w.len;
-    load_run<T, KIND>(x + row, c.ldx, ix, full, w.len - t - at, n, 0u, rx);
-    load_run<T, KIND>(g + row, c.ldx, ix, full, w.len - t - at, n, Word<T>::kPast, rg);
+    load_run<T, KIND>(x + row, c.ldx, ix, full, w.len - t - at, in, 0u, rx);
+    load_run<T, KIND>(g + row, c.ldx, ix, full, w.len - t - at, in, Word<T>::kPast, rg);
   };
   load_tile(tile0);
   for (int tile = tile0; tile < tile1; ++tile) {
@@ -319,7 +338,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     float a[K][V], b[K][V], A[V], B[V];
     u32x2 cx[K], cg[K];  // this tile's rows; the next ones are on their way from here on
 #pragma unroll
-    for (int k = 0; k < K; ++k) cx[k] = rx[k], cg[k] = rg[k];
+    for (int k = 0; k < K; ++k) cx[k] = in.take(rx[k]), cg[k] = in.take(rg[k]);
     if (tile + 1 < tile1) load_tile(tile + 1);
 #pragma unroll
     for (int v = 0; v < V; ++v) A[v] = 1.f, B[v] = 0.f;
@@ -390,7 +409,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 8)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int o = lane % L::LV * V, sub = lane / L::LV;
   const int n = c.dim - (w.col + o), own = w.col + (lane & (CH - 1));
-  const uint32_t col = n > 0 ? o : 0;
+  const Reads<T, KIND> in(o, n);
   float bias[V];
   load_bias<V>(c, w, w.col + o, bias);
   for (int tile = w.chunk * c.chunk; tile < min((w.chunk + 1) * c.chunk, c.tiles); ++tile) {
@@ -403,11 +422,11 @@ __global__ void __launch_bounds__(64 * kScanWaves, 8)
     const bool full = (tile + 1) * kScanTile <= w.len;
     const int live = w.len - tile * kScanTile - 32 * wave - sub * K;
     u32x2 rp[K], rg[K];
-    load_run<T, KIND>(p + row * ldp + w.col, ldp, (uint32_t)(sub * K * (int)ldp + (int)col) * (uint32_t)sizeof(T),
-                       full, live, n, 0u, rp);
-    load_run<T, KIND>(static_cast<const T*>(c.g) + row * c.ldx + w.col, c.ldx,
-                       (uint32_t)(sub * K * (int)c.ldx + (int)col) * (uint32_t)sizeof(T), full, live, n,
-                       Word<T>::kPast, rg);
+    load_run<T, KIND>(p + row * ldp + w.col - in.kBack, ldp,
+                      (uint32_t)(sub * K * (int)ldp + (int)in.col) * (uint32_t)sizeof(T), full, live, in, 0u, rp);
+    load_run<T, KIND>(static_cast<const T*>(c.g) + row * c.ldx + w.col - in.kBack, c.ldx,
+                      (uint32_t)(sub * K * (int)c.ldx + (int)in.col) * (uint32_t)sizeof(T), full, live, in,
+                      Word<T>::kPast, rg);
     float A[V], B[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) A[v] = 1.f, B[v] = 0.f;
@@ -415,8 +434,8 @@ __global__ void __launch_bounds__(64 * kScanWaves, 8)
     for (int q = 0; q < K; ++q) {
       const int k = REVERSE ? K - 1 - q : q;
       float pv[V], gv[V];
-      expand(rp[k], pv);
-      expand(rg[k], gv);
+      expand(in.take(rp[k]), pv);
+      expand(in.take(rg[k]), gv);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const Gate u = gate<sizeof(T) == 4>(gv[v] + bias[v]);
@@ -508,9 +527,10 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
   const int oc = lane & (CH - 1), own = w.col + oc;
   const bool keeper = wave == 0 && lane < CH && own < c.dim;
   const int64_t row0 = w.seq * c.T;
-  const T* x = static_cast<const T*>(c.x) + row0 * c.ldx + w.col;
-  const T* g = static_cast<const T*>(c.g) + row0 * c.ldx + w.col;
-  const T* d = dh + row0 * lddh + w.col;
+  const Reads<T, KIND> in(o, n);
+  const T* x = static_cast<const T*>(c.x) + row0 * c.ldx + w.col - in.kBack;
+  const T* g = static_cast<const T*>(c.g) + row0 * c.ldx + w.col - in.kBack;
+  const T* d = dh + row0 * lddh + w.col - in.kBack;
   T *dx0 = dx + row0 * c.ldx + w.col, *dg0 = dg + row0 * c.ldx + w.col;
   float bias[V];
   load_bias<V>(c, w, w.col + o, bias);
@@ -521,19 +541,19 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     else if (dh_last) mu = dh_last[w.seq * c.dim + own];
   }
   const int at = 32 * wave + sub * K;
-  const uint32_t col = n > 0 ? o : 0;
-  const uint32_t ix = (uint32_t)(sub * K * (int)c.ldx + (int)col) * (uint32_t)sizeof(T);
-  const uint32_t id = (uint32_t)(sub * K * (int)lddh + (int)col) * (uint32_t)sizeof(T);
+  const uint32_t ix = (uint32_t)(sub * K * (int)c.ldx + (int)in.col) * (uint32_t)sizeof(T);
+  const uint32_t id = (uint32_t)(sub * K * (int)lddh + (int)in.col) * (uint32_t)sizeof(T);
+  const uint32_t iw = KIND == kOdd ? (uint32_t)(sub * K * (int)c.ldx + o) * (uint32_t)sizeof(T) : ix;  // written
   u32x2 rx[K], rg[K], rd[K];
   float s = 0.f;
   auto load_tile = [&](int tile) {
     const int t = tile * kScanTile;
     const int64_t row = (int64_t)(t + 32 * wave) * c.ldx;
     const bool full = t + kScanTile <= w.len;
-    load_run<T, KIND>(x + row, c.ldx, ix, full, w.len - t - at, n, 0u, rx);
+    load_run<T, KIND>(x + row, c.ldx, ix, full, w.len - t - at, in, 0u, rx);
     s = own < c.dim ? states[(w.seq * c.tiles + tile) * c.dim + own] : 0.f;
-    load_run<T, KIND>(g + row, c.ldx, ix, full, w.len - t - at, n, Word<T>::kPast, rg);
-    load_run<T, KIND>(d + (int64_t)(t + 32 * wave) * lddh, lddh, id, full, w.len - t - at, n, 0u, rd);
+    load_run<T, KIND>(g + row, c.ldx, ix, full, w.len - t - at, in, Word<T>::kPast, rg);
+    load_run<T, KIND>(d + (int64_t)(t + 32 * wave) * lddh, lddh, id, full, w.len - t - at, in, 0u, rd);
   };
   load_tile(tile1 - 1);
   for (int tile = tile1 - 1; tile >= tile0; --tile) {
@@ -546,8 +566,8 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
 #pragma unroll
       for (int k = 0; k < K; ++k)
         if (n > 0 && t + k < c.T) {
-          store_row<T, KIND>(row_at(tx + k * c.ldx, ix), (u32x2){0u, 0u}, n);
-          store_row<T, KIND>(row_at(tg + k * c.ldx, ix), (u32x2){0u, 0u}, n);
+          store_row<T, KIND>(row_at(tx + k * c.ldx, iw), (u32x2){0u, 0u}, n);
+          store_row<T, KIND>(row_at(tg + k * c.ldx, iw), (u32x2){0u, 0u}, n);
         }
       if (part && sub == 0)
 #pragma unroll
@@ -560,7 +580,7 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
     u32x2 cx[K], cg[K], cd[K];  // this tile's rows; the next ones are on their way from here on
     const float here = s;
 #pragma unroll
-    for (int k = 0; k < K; ++k) cx[k] = rx[k], cg[k] = rg[k], cd[k] = rd[k];
+    for (int k = 0; k < K; ++k) cx[k] = in.take(rx[k]), cg[k] = in.take(rg[k]), cd[k] = in.take(rd[k]);
     if (tile > tile0) load_tile(tile - 1);
 #pragma unroll
     for (int v = 0; v < V; ++v) A[v] = 1.f, B[v] = R[v] = 0.f;
@@ -654,8 +674,8 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
 #pragma unroll
       for (int v = 0; v < V; ++v) sum[v] += og[v];
       if (n > 0 && (full || t + k < c.T)) {
-        store_row<T, KIND>(row_at(tx + k * c.ldx, ix), collapse(ox), n);
-        store_row<T, KIND>(row_at(tg + k * c.ldx, ix), collapse(og), n);
+        store_row<T, KIND>(row_at(tx + k * c.ldx, iw), collapse(ox), n);
+        store_row<T, KIND>(row_at(tg + k * c.ldx, iw), collapse(og), n);
       }
     }
     if (part) {
@@ -831,7 +851,8 @@ nbsgd_status fill_call(Call* c, const void* x, const void* g, int64_t ldx, int32
 // lines; `bytes`: what an unsplit call reads, against 1.5 times the memory-side cache.
 template <typename T, typename F>
 void by_kind(int dim, bool written, bool read, int64_t bytes, F f) {
-  if (dim % Lanes<T>::V) f(std::integral_constant<Kind, kOdd>());
+  if (dim < Lanes<T>::V) f(std::integral_constant<Kind, kTiny>());
+  else if (dim % Lanes<T>::V) f(std::integral_constant<Kind, kOdd>());
   else if (!written) f(std::integral_constant<Kind, kWhole>());
   else if (!read || bytes < (int64_t)384 << 20) f(std::integral_constant<Kind, kLines>());
   else f(std::integral_constant<Kind, kFar>());

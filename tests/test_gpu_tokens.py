@@ -286,6 +286,13 @@ def test_scan(n, m, b, T, C, joint, lengths, bias, h0, dtype):
     assert (G[:, :, off + C:] == SENTINEL).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("C", [1, 2, 3, 5, 6, 31, 33, 63, 65, 66, 67, 131])
+def test_scan_widths(C, dtype):
+    """Rows shorter than a lane's 8 bytes, and ones whose last lane has any part of them."""
+    test_scan(1, 2, 2, 290, C, C % 2, "ragged", 1, 1, dtype)
+
+
 def test_scan_extreme_gates():
     """Gates of 0 and 1, and infinite ones: the state is replaced, kept, and never NaN."""
     g = torch.tensor([float("inf"), -float("inf"), 200.0, -200.0, 88.0, -104.0, 1e38, -1e38], device=DEV)
