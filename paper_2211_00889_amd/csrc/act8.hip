@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(256)
 // loads go out a whole stage before they are wanted.  Of eight waves, two on each SIMD (waves w
 // and w + 4), the late half runs half a stage behind: while one wave of a SIMD multiplies, the
 // other one unpacks, turns and loads, and two barriers a stage keep it so.
-// 32 mini-batches of 4096 x 1024 x 2048: 482 us, 1.14 PFLOP/s (a library's bf16 product of
+// 32 mini-batches of 4096 x 1024 x 2048: 473-487 us, 1.13-1.16 PFLOP/s (a library's bf16 product of
 // 8192^3 reaches 1.17); 514 us over many passes, against 526 with both halves in step.  What
 // bounds it is power: 0.93 million cycles at 1.9 GHz, 0.52 of them the MFMAs' own, where both
 // halves in step and loads among the products took 1.21 million at 2.2 GHz.  Of the 514 us no
