@@ -202,8 +202,8 @@ __global__ void __launch_bounds__(256)
 // as both operands agree: of 64 tokens, octets 2 g of lanes g are step 0 and octets 2 g + 1 step 1,
 // so that
 //   A  (packed) is loaded 16 bytes a lane, 16 tokens of a channel, straight from memory, and
-//      made bf16 in registers, u * 2^k - 128 * 2^k of the byte with its top bit turned, exactly;
-//      every value once, since a wave has all columns of its channels
+//      made bf16 in registers, q * 2^k exactly; every value once, since
+//      a wave has all columns of its channels
 //   B  (dY) comes a row a token: a thread turns 4 tokens x 8 columns and writes 8 bytes a
 //      column to LDS, column 8 q + e of the tile to slot e * BN / 8 + q, so that the writes and
 //      the fragment reads are contiguous and a lane's results of eight (or four) fragments are
@@ -241,19 +241,16 @@ struct GradCall {
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
-// Eight bytes of a channel as bf16, on the step 2^(byte - 127).  A byte of 255 makes an infinite
-// step and NaNs of every value: inf - inf.
+// Eight bytes of a channel as bf16 on their step: q * 2^k exactly for every q and k, 127 * 2^121
+// included (with 128 added to the bytes and its product taken off again, 128 * 2^121 is no fp32).
 __device__ __forceinline__ bf16x8 unpack8(uint32_t q0, uint32_t q1, float step) {
-  const float back = -128.f * step;
-  const uint32_t q[2] = {q0 ^ 0x80808080u, q1 ^ 0x80808080u};
+  const uint32_t q[2] = {q0, q1};
   u32x4 r;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const uint32_t u = q[h];
-    const float f0 = fmaf((float)(u & 0xffu), step, back), f1 = fmaf((float)(u >> 8 & 0xffu), step, back);
-    const float f2 = fmaf((float)(u >> 16 & 0xffu), step, back), f3 = fmaf((float)(u >> 24), step, back);
-    r[2 * h] = pack2(f0, f1);
-    r[2 * h + 1] = pack2(f2, f3);
+    r[2 * h] = pack2((float)(int8_t)u * step, (float)(int8_t)(u >> 8) * step);
+    r[2 * h + 1] = pack2((float)(int8_t)(u >> 16) * step, (float)(int8_t)(u >> 24) * step);
   }
   return __builtin_bit_cast(bf16x8, r);
 }
@@ -348,7 +345,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
   auto make_a = [&](int st) {
 #pragma unroll
     for (int a = 0; a < MT; ++a) {
-      const float step = __builtin_bit_cast(float, (sa[a] >> (16 * (st & 1) + 8 * (g >> 1)) & 0xffu) << 23);
+      const float step = step_of(sa[a] >> (16 * (st & 1) + 8 * (g >> 1)) & 0xffu);
       A[0][a] = unpack8(qa[a][0], qa[a][1], step);
       A[1][a] = unpack8(qa[a][2], qa[a][3], step);
     }
