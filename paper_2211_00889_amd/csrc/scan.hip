@@ -24,6 +24,11 @@
 
 using namespace nbsgd;
 
+// A tile's composition is computed by k_scan_pairs in a call that splits its sequences and by k_scan or
+// k_scan_grad in one that does not, and has to be the same bit for bit: the maps' products and sums
+// stand in one order in both, and where one is fused is written out, not left to the compiler.
+#pragma clang fp contract(off)
+
 namespace {
 
 // Gate a = sigmoid(z) and its complement, both accurate where they are small (1 - a would
@@ -427,9 +432,9 @@ __global__ void __launch_bounds__(64 * kScanWaves, 8)
     load_run<T, KIND>(static_cast<const T*>(c.g) + row * c.ldx + w.col - in.kBack, c.ldx,
                       (uint32_t)(sub * K * (int)c.ldx + (int)in.col) * (uint32_t)sizeof(T), full, live, in,
                       Word<T>::kPast, rg);
-    float A[V], B[V];
+    float A[V], B[V], last[V];  // last: the gate before
 #pragma unroll
-    for (int v = 0; v < V; ++v) A[v] = 1.f, B[v] = 0.f;
+    for (int v = 0; v < V; ++v) A[v] = last[v] = 1.f, B[v] = 0.f;
 #pragma unroll
     for (int q = 0; q < K; ++q) {
       const int k = REVERSE ? K - 1 - q : q;
@@ -439,9 +444,14 @@ __global__ void __launch_bounds__(64 * kScanWaves, 8)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const Gate u = gate<sizeof(T) == 4>(gv[v] + bias[v]);
-        B[v] = REVERSE ? u.a * (pv[v] + B[v]) : fmaf(u.a, B[v], u.rest * pv[v]);
+        B[v] = REVERSE ? fmaf(last[v], B[v], pv[v]) : fmaf(u.a, B[v], u.rest * pv[v]);
         A[v] *= u.a;
+        last[v] = u.a;
       }
+    }
+    if (REVERSE) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) B[v] *= last[v];
     }
     float EA[V], EB[V];
     compose<T, !REVERSE>(sub, A, B, EA, EB);
@@ -595,18 +605,20 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
         a[k][v] = u.a;
         rest[k][v] = u.rest;
         B[v] = fmaf(u.a, B[v], u.rest * xv[v]);
-        A[v] *= u.a;
       }
     }
 #pragma unroll
-    for (int k = K - 1; k >= 0; --k) {
+    for (int k = K - 1; k >= 0; --k) {  // as in k_scan_pairs
       float dv[V];
       expand(again(cd[k]), dv);
 #pragma unroll
-      for (int v = 0; v < V; ++v) R[v] = a[k][v] * (dv[v] + R[v]);
+      for (int v = 0; v < V; ++v) {
+        R[v] = fmaf(k == K - 1 ? 1.f : a[min(k + 1, K - 1)][v], R[v], dv[v]);
+        A[v] *= a[k][v];
+      }
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v) RA[v] = A[v];
+    for (int v = 0; v < V; ++v) RA[v] = A[v], R[v] *= a[0][v];
     float EA[V], EB[V], FA[V], FR[V];
     compose<T, false>(sub, RA, R, FA, FR);
     if (sub == 0) {
@@ -662,10 +674,9 @@ __global__ void __launch_bounds__(64 * kScanWaves, 2)
       expand(again(cd[k]), dv);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const float lam = dv[v] + m[v];
-        ox[v] = lam * rest[k][v];
+        m[v] = fmaf(k == K - 1 ? 1.f : a[min(k + 1, K - 1)][v], m[v], dv[v]);  // l of token k
+        ox[v] = m[v] * rest[k][v];
         og[v] = ox[v] * a[k][v] * gap[k][v];
-        m[v] = a[k][v] * lam;
       }
       if (!full && t + k >= w.len) {  // whatever comes from behind stays behind
 #pragma unroll

@@ -9,7 +9,7 @@ from oracle import tokens as orc
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from tests.test_gpu_tokens import BF16, DEV, SENTINEL, _close, _np, _say, _ws  # noqa: E402
+from tests.test_gpu_tokens import BF16, DEV, F32, SENTINEL, _close, _np, _say, _ws  # noqa: E402
 
 
 # --------------------------------------------- 8-bit weight gradient, its range
@@ -89,3 +89,69 @@ def test_act_grad_of_nan_blocks(n, m, T, dim, out):
         assert torch.isnan(got[sorted(bad)]).all()
         want, bound = orc.act_grad((q * step)[:, others], _np(dY[i, j]))
         _close("G", got[torch.from_numpy(others).to(DEV)], want, bound)
+
+
+# ------------------------------------------------- a mini-batch's results are its own
+def _bits(t):
+    return t.contiguous().view(torch.int32 if t.dtype is F32 else torch.int16)
+
+
+def _scan_both(x, g, dh, X, h0, dl, lengths):
+    """Every output of the two passes."""
+    n, m, b, T, C = x.shape
+    mask, ws = np.ones((n, m), np.uint8), _ws(nb.scan_workspace_bytes(n, m, b, T, C))
+    o = {k: torch.empty_like(x) for k in ("h", "dx", "dg")}
+    o["last"], o["dh0"] = torch.empty_like(h0), torch.empty_like(h0)
+    o["states"] = torch.empty((n, m, b, -(-T // nb.SCAN_INTERVAL), C), device=DEV)
+    o["G"] = torch.zeros((n, m, X.shape[1]), device=DEV)
+    nb.scan(x, g, mask, o["h"], X=X, h0=h0, h_last=o["last"], lengths=lengths, states=o["states"], workspace=ws)
+    nb.scan_grad(x, g, o["states"], dh, mask, o["dx"], o["dg"], ws, X=X, G=o["G"], dh_last=dl, dh0=o["dh0"], lengths=lengths)
+    return o
+
+
+def _scan_some(seed, n, m, b, T, C, dtype):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    shape = (n, m, b, T, C)
+    x, g, dh = (torch.randn(shape, generator=gen, device=DEV, dtype=F32 if dtype is F32 else BF16) for _ in range(3))
+    h0, dl = (torch.randn((n, m, b, C), generator=gen, device=DEV) for _ in range(2))
+    X = torch.randn((n, (C + 3) // 4 * 4), generator=gen, device=DEV) + 2
+    lengths = torch.randint(0, T + 1, (n, m, b), generator=gen, device=DEV, dtype=torch.int32)
+    lengths[..., 0] = T
+    return x, g, dh, X, h0, dl, lengths
+
+
+def _against_oracle(o, data, at, few, dtype):
+    """One sequence's channels `few` of every output."""
+    x, g, dh, X, h0, dl, lengths = data
+    L = int(lengths[at])
+    args = [_np(x[at][..., few]), _np(g[at][..., few]), _np(X[at[0], few]), _np(h0[at][few]), L]
+    (ho, before, s), (eh, eb, es) = orc.scan(*args)
+    _close("h", o["h"][at][..., few], ho, eh, dtype)
+    _close("h_last", o["last"][at][few], s, es)
+    _close("states", o["states"][at][..., few], before[::nb.SCAN_INTERVAL], eb[::nb.SCAN_INTERVAL])
+    (gx, gg, g0, _), (ex, eg, e0, _) = orc.scan_grad(*args, _np(dh[at][..., few]), _np(dl[at][few]))
+    _close("dx", o["dx"][at][..., few], gx, ex, dtype)
+    _close("dg", o["dg"][at][..., few], gg, eg, dtype)
+    _close("dh0", o["dh0"][at][few], g0, e0)
+
+
+@pytest.mark.parametrize("n,m,b,T,C,dtype", [
+    # walked whole with the others; alone a tile a workgroup, or three and two (the last ones)
+    (4, 4, 8, 700, 136, F32), (4, 4, 8, 700, 198, BF16), (4, 8, 8, 520, 1024, BF16), (4, 1, 2, 5000, 4096, BF16),
+    (4, 2, 2, 5000, 1030, F32),
+])
+def test_scan_of_many_and_alone(n, m, b, T, C, dtype):
+    """One mini-batch of a call whose sequences are walked whole, against the same one in a call that
+    splits them: bit for bit."""
+    _say(f"scan many and alone {n}x{m}x{b} T={T} dim={C} {dtype}")
+    data = _scan_some(T + C, n, m, b, T, C, dtype)
+    x, g, dh, X, h0, dl, lengths = data
+    lengths[n - 1, 0, 1] = 2 * T // 3
+    whole = _scan_both(*data)
+    for i, j in ((0, 0), (n - 1, m - 1)):
+        own = [t[i:i + 1, j:j + 1].contiguous() for t in (x, g, dh)]
+        one = _scan_both(*own, X[i:i + 1].contiguous(), *(t[i:i + 1, j:j + 1].contiguous() for t in (h0, dl, lengths)))
+        differ = {k: int((_bits(one[k][0, 0]) != _bits(whole[k][i, j])).sum()) for k in one}
+        assert not any(differ.values()), differ
+    _against_oracle(whole, data, (n - 1, 0, 1), slice(C - 9, C), dtype)
+    _against_oracle(whole, data, (0, 0, 0), slice(0, 7), dtype)
