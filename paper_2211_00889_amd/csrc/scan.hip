@@ -419,9 +419,9 @@ __global__ void __launch_bounds__(64 * kScanWaves, 8)
   load_bias<V>(c, w, w.col + o, bias);
   for (int tile = w.chunk * c.chunk; tile < min((w.chunk + 1) * c.chunk, c.tiles); ++tile) {
     const int64_t row = w.seq * c.T + tile * kScanTile + 32 * wave;
-    if (tile * kScanTile >= w.len) {  // uniform: behind the sequence
+    if (tile * kScanTile >= w.len) {  // uniform: behind the sequence; 1 s + -0 is s, of -0 too
       if (wave == 0 && lane < CH && own < c.dim)
-        *reinterpret_cast<f32x2*>(pairs + 2 * ((w.seq * c.tiles + tile) * c.dim + own)) = (f32x2){1.f, 0.f};
+        *reinterpret_cast<f32x2*>(pairs + 2 * ((w.seq * c.tiles + tile) * c.dim + own)) = (f32x2){1.f, -0.f};
       continue;
     }
     const bool full = (tile + 1) * kScanTile <= w.len;

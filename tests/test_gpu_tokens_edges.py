@@ -155,3 +155,18 @@ def test_scan_of_many_and_alone(n, m, b, T, C, dtype):
         assert not any(differ.values()), differ
     _against_oracle(whole, data, (n - 1, 0, 1), slice(C - 9, C), dtype)
     _against_oracle(whole, data, (0, 0, 0), slice(0, 7), dtype)
+
+
+@pytest.mark.parametrize("T", [12, 300, 1500])
+def test_a_state_keeps_its_sign(T):
+    """A state of -0 of an ended sequence, in a call that walks its sequences whole and in one that
+    splits them, forward and backward."""
+    n, m, b, C = 8, 8, 8, 4
+    x, g, dh, X, h0, dl, lengths = _scan_some(T, n, m, b, T, C, F32)
+    h0.fill_(-0.0), dl.fill_(-0.0), lengths.zero_()
+    whole = _scan_both(x, g, dh, X, h0, dl, lengths)
+    one = _scan_both(*(t[:1, :1].contiguous() for t in (x, g, dh)), X[:1].contiguous(),
+                     *(t[:1, :1].contiguous() for t in (h0, dl, lengths)))
+    for o in (whole, one):
+        for k in ("last", "dh0", "states"):
+            assert torch.equal(_bits(o[k]), _bits(torch.full_like(o[k], -0.0))), k
