@@ -467,7 +467,8 @@ nbsgd_status nbsgd_embed(const float *E, int64_t ld, int32_t n, int32_t m, int32
 /* Gradient of the lookup, every row of the table written:
  *   G[i][j][v][:] = scale * sum_{t : tokens[i][j][t] == v} dY[i][j][t][:]
  * A row's sum runs over its own tokens in an order that the tokens alone fix; no
- * atomics.  Rows of dY whose token lies outside [0, vocab) are not read.
+ * atomics.  A row without tokens is 0 whatever scale is.  Rows of dY whose token lies
+ * outside [0, vocab) are not read.
  * G  device fp32, the gradient of mini-batch (i, j) at G + (i*m + j)*ld
  * workspace  nbsgd_embed_workspace_bytes(n, m, T, vocab, dim)             */
 nbsgd_status nbsgd_embed_workspace_bytes(int32_t n, int32_t m, int32_t T, int32_t vocab,

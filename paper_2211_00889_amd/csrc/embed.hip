@@ -352,6 +352,10 @@ __global__ void __launch_bounds__(256)
       }
     }
     if (v + team >= v1) continue;
+    uint64_t any = 0;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) any |= hit[q];
+    const float scale = any ? c.scale : 0.f;  // a row without tokens is 0, of an infinite scale too
     float* to = c.G + id * c.ld + (int64_t)(v + team) * c.dim;
     for (int col = V * (lane % c.L); col < c.dim; col += V * c.L) {
       const int n = min(V, c.dim - col);
@@ -379,7 +383,7 @@ __global__ void __launch_bounds__(256)
         }
       }
 #pragma unroll
-      for (int v4 = 0; v4 < V; ++v4) sum[v4] *= c.scale;
+      for (int v4 = 0; v4 < V; ++v4) sum[v4] *= scale;
       store_row4(to + col, n, sum);
     }
   }

@@ -9,7 +9,7 @@ from oracle import tokens as orc
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from tests.test_gpu_tokens import BF16, DEV, F32, SENTINEL, _close, _np, _say, _ws  # noqa: E402
+from tests.test_gpu_tokens import BF16, DEV, F32, SENTINEL, _close, _np, _rows, _say, _ws  # noqa: E402
 
 
 # --------------------------------------------- 8-bit weight gradient, its range
@@ -170,3 +170,24 @@ def test_a_state_keeps_its_sign(T):
     for o in (whole, one):
         for k in ("last", "dh0", "states"):
             assert torch.equal(_bits(o[k]), _bits(torch.full_like(o[k], -0.0))), k
+
+
+# ------------------------------------------------------------------ embeddings
+@pytest.mark.parametrize("T", [5, 128, 129, 1500])
+@pytest.mark.parametrize("scale", [float("inf"), float("nan"), -2.0, 0.0])
+def test_rows_without_tokens_are_zero(T, scale):
+    """Whatever the scale is, and +0: a few tokens and sorted ones alike."""
+    rng = np.random.default_rng(T)
+    V, D = 300, 21
+    tok = rng.integers(0, V // 2, (1, 1, T)).astype(np.int32)
+    dY, _ = _rows((1, 1, T, D), F32, rng=rng)
+    G = torch.full((1, 1, (V * D + 3) // 4 * 4), SENTINEL, device=DEV)
+    nb.embed_grad(dY, torch.from_numpy(tok).to(DEV), [[1]], G, 0, V, _ws(nb.embed_workspace_bytes(1, 1, T, V, D)), scale=scale)
+    rows = G[0, 0, :V * D].view(V, D)
+    empty = torch.from_numpy(~np.isin(np.arange(V), tok)).to(DEV)
+    assert (_bits(rows[empty]) == 0).all()
+    if np.isfinite(scale):
+        want, bound = orc.embed_grad(_np(dY[0, 0]), tok[0, 0], V, scale)
+        _close("G", rows, want, bound)
+    else:
+        assert not torch.isfinite(rows[~empty]).any()
