@@ -233,7 +233,7 @@ struct GradCall {
   int64_t ldy, ld;  // of out: floats from one mini-batch to the next
   int64_t part;     // floats from one part to the next
   int32_t T, dim, cols, parts, per;  // per: blocks of a part, a multiple of four
-  int32_t batches, border;           // mini-batches of dY; tokens that seven elements follow
+  int32_t border;                    // act8_border
   int32_t tm, tn, items;
   Act8 lay;
   Groups groups;
@@ -291,10 +291,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_act8_grad(GradCall c) {
 
   u32x4 qa[MT], rb[4];
   uint32_t sa[MT];
-  // The first `plain` stages are read without looking: all their tokens are there, and seven elements
-  // behind the last one's row
-  const int sure = c0 + BN <= c.cols || id + 1 < c.batches ? tokens : min(tokens, c.border);
-  const int plain = max(0, sure / kActBlock - blk0) / kHB;
+  // the first `plain` stages are read without looking
+  const int plain = max(0, act8_sure(tokens, c.border, c0, BN, c.cols) / kActBlock - blk0) / kHB;
   auto load_rows = [&](int st) {
     const uint8_t* from = reinterpret_cast<const uint8_t*>(rows + (int64_t)(blk0 + kHB * st) * kActBlock * c.ldy);
 #pragma unroll
@@ -585,8 +583,7 @@ extern "C" nbsgd_status nbsgd_act_grad(const void* packed, const void* dY, int64
   c.T = T;
   c.dim = dim;
   c.cols = out;
-  c.batches = n * m;
-  c.border = T - (int32_t)ceil_div(7, ldy);
+  c.border = act8_border(T, ldy);
   c.parts = act8_splits(T, dim, out);
   c.per = (int32_t)(ceil_div(ceil_div(lay.blocks, c.parts), 4) * 4);
   c.lay = lay;

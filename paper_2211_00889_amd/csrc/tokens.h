@@ -8,6 +8,12 @@
 
 #include "nbsgd.h"
 
+#ifdef __HIPCC__
+#define NBSGD_HD __host__ __device__ __forceinline__
+#else
+#define NBSGD_HD inline
+#endif
+
 namespace nbsgd {
 
 constexpr int kMaxGroups = NBSGD_MAX_LEARNERS * NBSGD_MAX_MINIBATCHES;
@@ -90,6 +96,16 @@ inline Act8 act8_layout(int64_t T, int64_t dim) {
   return a;
 }
 nbsgd_status check_act8(int32_t T, int32_t dim);
+// A tile of the weight gradient, columns c0 .. c0 + width of `cols`, reads rows of dY without looking
+// at their ends, eight elements from every eighth column: up to seven of them follow the row's last.
+// Where there are any they have to be the same mini-batch's, since the next one may be unfinished and is
+// not read then: those of tokens below act8_border are.  The number of the first `tokens` tokens that
+// are read so:
+inline int32_t act8_border(int32_t T, int64_t ldy) { return T - (int32_t)ceil_div(7, ldy); }
+NBSGD_HD int act8_sure(int tokens, int border, int c0, int width, int cols) {
+  const bool ends = c0 + width <= cols || cols % 8 == 0;  // every load with its row, or before
+  return ends || tokens < border ? tokens : border;
+}
 // Parts that the tokens of a weight gradient are summed in, by workgroups of their own where
 // its smallest tiles (64 x 128) are few and the tokens many.  By the mini-batch's sizes alone,
 // not by how many mini-batches a call has, so that a result does not depend on the others.
