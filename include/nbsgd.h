@@ -517,6 +517,9 @@ nbsgd_status nbsgd_scan(const void *x, const void *g, int64_t ldx, int32_t dtype
  *   l_t = dh_t + a_{t+1} l_{t+1}   (from dh_last after the last token)
  *   dx_t = l_t (1 - a_t)           dg_t = l_t (h_{t-1} - x_t) a_t (1 - a_t)
  *   dh0 = a_1 l_1                  Gbias = sum over the mini-batch's tokens of dg_t
+ * An infinite or NaN dh or dh_last makes a channel's gradients of its token and of the
+ * ones before it infinite or NaN, not always as the formula has them; an x or h_0
+ * makes so those of g from its token on, and Gbias.
  * x, g, bias, lengths, mask  as in the forward call; states its output
  * dh       [n][m][batch][T] rows, lddh >= dim apart; not read past a length
  * dh_last  device fp32 [n][m][batch][dim], or NULL: zero

@@ -9,7 +9,7 @@ from oracle import tokens as orc
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from tests.test_gpu_tokens import BF16, DEV, F32, SENTINEL, _close, _np, _rows, _say, _ws  # noqa: E402
+from tests.test_gpu_tokens import BF16, DEV, F32, SENTINEL, _close, _np, _rows, _say, _tokens, _ws  # noqa: E402
 
 
 # --------------------------------------------- 8-bit weight gradient, its range
@@ -191,3 +191,88 @@ def test_rows_without_tokens_are_zero(T, scale):
         _close("G", rows, want, bound)
     else:
         assert not torch.isfinite(rows[~empty]).any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind,T,vocab,dim", [("zipf", 40001, 300, 5), ("uniform", 33000, 70000, 3), ("one", 50000, 9, 4),
+                                              ("zipf", 32768, 5000, 8), ("uniform", 262144, 40, 2)])
+def test_embed_grad_of_many_tokens(kind, T, vocab, dim, dtype):
+    """More than four sorted runs to join."""
+    rng = np.random.default_rng(T)
+    _say(f"embed_grad {kind} T={T} vocab={vocab} dim={dim} {dtype}")
+    tok = _tokens(rng, kind, (1, 1, T), vocab)
+    dY, _ = _rows((1, 1, T, dim), dtype, rng=rng)
+    G = torch.full((1, 1, (vocab * dim + 3) // 4 * 4), SENTINEL, device=DEV)
+    nb.embed_grad(dY, torch.from_numpy(tok).to(DEV), [[1]], G, 0, vocab, _ws(nb.embed_workspace_bytes(1, 1, T, vocab, dim)))
+    want, bound = orc.embed_grad(_np(dY[0, 0]), tok[0, 0], vocab, 1.0)
+    _close("G", G[0, 0, :vocab * dim].view(vocab, dim), want, bound)
+
+
+# -------------------------------------------------- sequences of many tiles
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,m,b,T,C,ends", [
+    # 64 tiles, 65, 79: one and two rounds of the tiles' states; then two tiles a workgroup
+    (1, 1, 1, 16384, 7, ()), (1, 1, 2, 16385, 24, (16384,)), (1, 1, 3, 20000, 64, (17001, 3)),
+    (1, 2, 32, 5000, 40, (4999, 257, 256, 0, 1300)),
+])
+def test_scan_of_many_tiles(n, m, b, T, C, ends, dtype):
+    """More tiles than one round of the tiles' states takes, and more than one tile a workgroup, with
+    lengths that end inside them."""
+    _say(f"scan many tiles {n}x{m}x{b} T={T} dim={C} {dtype}")
+    data = _scan_some(T, n, m, b, T, C, dtype)
+    lengths = data[-1]
+    for k, e in enumerate(ends):
+        lengths[n - 1, m - 1, k + 1] = e
+    o = _scan_both(*data)
+    for k in range(min(b, len(ends) + 1)):
+        _against_oracle(o, data, (n - 1, m - 1, k), slice(max(0, C - 5), C), dtype)
+
+
+# ------------------------------------------------ infinities and NaNs in live values
+BAD = [float("inf"), -float("inf"), float("nan")]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,at", [(12, 5), (200, 70), (600, 258), (600, 0), (600, 599)])
+def test_infinities_stay_behind_their_token(T, at, dtype):
+    """An infinite or NaN x, h0, dh or dh_last: forward the tokens before it, backward the ones after it,
+    and every other channel are as the formula has them."""
+    _say(f"infinities T={T} at={at} {dtype}")
+    C = 9
+    data = _scan_some(T, 1, 1, 1, T, C, dtype)
+    x, g, dh, X, h0, dl, lengths = data
+    finite = [t.clone() for t in data]
+    want, none = _scan_both(*finite), slice(6, C)
+
+    def same(a, b):
+        assert torch.equal(_bits(a), _bits(b))
+
+    for c, v in enumerate(BAD):
+        x[0, 0, 0, at, c] = v
+        h0[0, 0, 0, 3 + c] = v
+    got = _scan_both(*data)
+    for k in want:
+        if k != "G":
+            same(got[k][..., none], want[k][..., none])
+    same(got["G"][..., none.start:C], want["G"][..., none.start:C])
+    same(got["h"][0, 0, 0, :at, :3], want["h"][0, 0, 0, :at, :3])
+    same(got["dg"][0, 0, 0, :at, :3], want["dg"][0, 0, 0, :at, :3])
+    for k in ("dx", "dh0"):  # x and h0 are not in them
+        same(got[k], want[k])
+    assert not torch.isfinite(got["h"][0, 0, 0, at:, :3].float()).any() and not torch.isfinite(got["last"][..., :6]).any()
+    assert not torch.isfinite(got["h"][0, 0, 0, :, 3:6].float()).any() and not torch.isfinite(got["G"][..., :6]).any()
+
+    x, g, dh, X, h0, dl, lengths = data = finite
+    for c, v in enumerate(BAD):
+        dh[0, 0, 0, at, c] = v
+        dl[0, 0, 0, 3 + c] = v
+    got = _scan_both(*data)
+    for k in ("h", "last", "states"):
+        same(got[k], want[k])
+    for k in ("dx", "dg", "dh0", "G"):
+        same(got[k][..., none], want[k][..., none])
+    for k in ("dx", "dg"):
+        same(got[k][0, 0, 0, at + 1:, :3], want[k][0, 0, 0, at + 1:, :3])
+    assert not torch.isfinite(got["dx"][0, 0, 0, :at + 1, :3].float()).any()
+    assert not torch.isfinite(got["dx"][0, 0, 0, :, 3:6].float()).any()
+    assert not torch.isfinite(got["dh0"][..., :6]).any() and not torch.isfinite(got["G"][..., :6]).any()
