@@ -34,7 +34,12 @@ namespace {
 // Gate a = sigmoid(z) and its complement, both accurate where they are small (1 - a would
 // cancel): with e = exp(-|z|) the larger is 1 / (1 + e) and the smaller e / (1 + e).  e is
 // 2^(-|z| log2 e) on the hardware's exponential; EXACT (fp32 rows) adds what the product's and
-// the constant's rounding lost (|z| 2^-24 of the value otherwise, below bf16's own step).
+// the constant's rounding lost and refines the reciprocal.  Of bf16 rows the smaller one may be off by
+// (1.25 |z| + 6) 2^-24 of its value, in h_last, states, dh0 and the bias's gradient too, which are
+// fp32; the larger one is taken as 1 - e r, to half a step but for the smaller one's error: a long
+// sequence keeps products of gates near 1, and 1 / (1 + e) as the hardware has it lost half of the
+// exact bits of dh0 that this keeps (17,384 tokens: 8.6e-7 off, 2.2e-7 so).  EXACT for bf16 too took 652 us
+// of 36 mini-batches of four sequences of 2048 x 1024 backward, this 620, neither 617.
 struct Gate {
   float a, rest;
 };
@@ -52,6 +57,7 @@ __device__ __forceinline__ Gate gate(float z) {
   float r = __builtin_amdgcn_rcpf(d);
   if constexpr (EXACT) r = fmaf(fmaf(-d, r, 1.f), r, r);  // the reciprocal's last place
   const float s = e * r;
+  if constexpr (!EXACT) r = fmaf(-e, r, 1.f);
   return z >= 0.f ? Gate{r, s} : Gate{s, r};
 }
 

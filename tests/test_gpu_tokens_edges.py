@@ -228,6 +228,28 @@ def test_scan_of_many_tiles(n, m, b, T, C, ends, dtype):
         _against_oracle(o, data, (n - 1, m - 1, k), slice(max(0, C - 5), C), dtype)
 
 
+# ------------------------------------------------------------ gates in 32 bits
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T", [1, 40])
+def test_gates_in_32_bits(T, dtype):
+    """The state after one token from a state of 1 and an x of 0 is the gate, in fp32 of bf16 rows too.
+    With u = 2^-24: the exponential's argument is off by |z| u (a product) and 0.25 |z| u (log2 e), it by 2 u
+    (its last place), 1 + e by u, the reciprocal by 2 u, a product by u.  So the smaller of gate and
+    complement is off by (1.25 |z| + 6) u of its value, and the larger, bf16 rows' 1 - e r, by that and half
+    a step of [1/2, 1]; fp32 rows' 1 / (1 + e) by the rounding of 1 + e, u of the value, besides."""
+    C = 4096
+    g = torch.linspace(-20, 20, C, device=DEV).to(dtype).view(1, 1, 1, 1, C).expand(1, 1, 1, T, C).contiguous()
+    h, last = torch.empty_like(g), torch.empty((1, 1, 1, C), device=DEV)
+    one = torch.ones((1, 1, 1), dtype=torch.int32, device=DEV)
+    nb.scan(torch.zeros_like(g), g, [[1]], h, h0=torch.ones_like(last), h_last=last, lengths=one,
+            workspace=_ws(nb.scan_workspace_bytes(1, 1, 1, T, C)))
+    z = _np(g[0, 0, 0, 0])
+    want, small = 1 / (1 + np.exp(-z)), 1 / (1 + np.exp(np.abs(z)))
+    room = small * (1.25 * np.abs(z) + 6) * orc.U + np.where(z > 0, orc.U / 2 + (orc.U * want if dtype is F32 else 0), 0)
+    off = np.abs(_np(last[0, 0, 0]) - want) / room
+    assert off.max() <= 1, (off.max(), z[off.argmax()], int((off > 1).sum()))
+
+
 # ------------------------------------------------ infinities and NaNs in live values
 BAD = [float("inf"), -float("inf"), float("nan")]
 
