@@ -298,3 +298,166 @@ def test_infinities_stay_behind_their_token(T, at, dtype):
     assert not torch.isfinite(got["dx"][0, 0, 0, :at + 1, :3].float()).any()
     assert not torch.isfinite(got["dx"][0, 0, 0, :, 3:6].float()).any()
     assert not torch.isfinite(got["dh0"][..., :6]).any() and not torch.isfinite(got["G"][..., :6]).any()
+
+
+# --------------------------------------------------------------- the limits of the sizes
+def test_a_sequence_of_the_longest_length():
+    """2^24 tokens with gates of 1/2, which a first-order filter computes.  A step adds at most 12 u of its
+    two terms (a gate of z = 0 is off by 10 u in the oracle's bound, a product and a sum by u each), half
+    of which the next one keeps: 24 u of the largest value."""
+    signal = pytest.importorskip("scipy.signal")
+    T = 1 << 24
+    _say("scan T=2^24")
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x, dh = (torch.randn((1, 1, 1, T, 1), generator=gen, device=DEV) for _ in range(2))
+    g, h, dx, dg = torch.zeros_like(x), *(torch.empty_like(x) for _ in range(3))
+    states, last = torch.empty((1, 1, 1, T // nb.SCAN_INTERVAL, 1), device=DEV), torch.empty((1, 1, 1, 1), device=DEV)
+    ws, G = _ws(nb.scan_workspace_bytes(1, 1, 1, T, 1)), torch.zeros((1, 1, 4), device=DEV)
+    nb.scan(x, g, [[1]], h, h_last=last, states=states, workspace=ws)
+    nb.scan_grad(x, g, states, dh, [[1]], dx, dg, ws, G=G)
+    v, d = _np(x).ravel(), _np(dh).ravel()
+    want = signal.lfilter([0.5], [1, -0.5], v)
+    lam = signal.lfilter([1], [1, -0.5], d[::-1])[::-1]
+    before = np.concatenate(([0.0], want[:-1]))
+    eh, el = 24 * orc.U * np.abs(v).max(), 24 * orc.U * 2 * np.abs(d).max()
+    _close("h", h.ravel(), want, eh)
+    _close("h_last", last.ravel(), want[-1:], eh)
+    _close("states", states.ravel(), before[::nb.SCAN_INTERVAL], eh)
+    _close("dx", dx.ravel(), lam / 2, el)
+    gap = before - v
+    # a factor each: l, the two gates (10 u each) with three products, h - x
+    eg = (el * np.abs(gap) + np.abs(lam) * (eh + orc.U * np.abs(gap))) / 4 + 23 * orc.U * np.abs(lam * gap) / 4
+    _close("dg", dg.ravel(), lam * gap / 4, eg)
+    _close("dbias", G[0, 0, :1], (lam * gap / 4).sum(keepdims=True), (eg + T * orc.U * np.abs(lam * gap) / 4).sum(keepdims=True))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_the_widest_rows(dtype):
+    C, T = 65536, 3
+    _say(f"rows of {C} {dtype}")
+    data = _scan_some(3, 1, 2, 1, 20, C, dtype)
+    o = _scan_both(*data)
+    for few in (slice(0, 5), slice(C - 5, C)):
+        _against_oracle(o, data, (0, 1, 0), few, dtype)
+    rng = np.random.default_rng(2)
+    X = torch.from_numpy(rng.normal(size=(1, 4 * C)).astype(np.float32)).to(DEV)
+    tok = np.array([[[3, 0, 3]]], np.int32)
+    Y = torch.empty((1, 1, T, C), dtype=dtype, device=DEV)
+    nb.embed(X, 0, 4, torch.from_numpy(tok).to(DEV), [[1]], Y, scale=0.5)
+    want = orc.embed(_np(X[0]).reshape(4, C), tok[0, 0], 0.5)
+    _close("Y", Y[0, 0], want, orc.U * np.abs(want), dtype)
+    for reps in (1, 50):  # few tokens and sorted ones
+        t = np.tile(tok, (1, 1, reps))
+        dY, _ = _rows((1, 1, T * reps, C), dtype, rng=rng)
+        G = torch.full((1, 1, 4 * C), SENTINEL, device=DEV)
+        nb.embed_grad(dY, torch.from_numpy(t).to(DEV), [[1]], G, 0, 4, _ws(nb.embed_workspace_bytes(1, 1, T * reps, 4, C)))
+        want, bound = orc.embed_grad(_np(dY[0, 0]), t[0, 0], 4, 1.0)
+        _close("G", G[0, 0].view(4, C), want, bound)
+    for dim, out in ((C, 6), (6, C)):
+        A, _ = _rows((1, 1, 70, dim), dtype, rng=rng)
+        dY, _ = _rows((1, 1, 70, out), BF16, rng=rng)
+        packed = torch.empty((1, 1, nb.act_bytes(70, dim)), dtype=torch.uint8, device=DEV)
+        back = torch.empty((1, 1, 70, dim), device=DEV)
+        nb.act_pack(A, [[1]], packed)
+        nb.act_unpack(packed, [[1]], back)
+        q, step = _act8(_np(A[0, 0]))
+        assert np.array_equal(_np(back[0, 0]), q * step)
+        G = torch.empty((1, 1, dim * out), device=DEV)
+        nb.act_grad(packed, dY, [[1]], G, 0, dim, _ws(nb.act_workspace_bytes(1, 1, 70, dim, out)))
+        want, bound = orc.act_grad(q * step, _np(dY[0, 0]))
+        _close("G", G[0, 0].view(dim, out), want, bound)
+
+
+@pytest.mark.parametrize("T", [100, 300])
+def test_the_largest_vocabulary(T):
+    V, D = 1 << 24, 4
+    _say(f"vocabulary of 2^24, {T} tokens")
+    rng = np.random.default_rng(T)
+    tok = rng.integers(0, V, (1, 1, T)).astype(np.int32)
+    tok[0, 0, :6] = [V - 1, 0, V - 1, -1, V, 2 ** 31 - 1]
+    dY, _ = _rows((1, 1, T, D), F32, rng=rng)
+    G = torch.full((1, 1, V * D), SENTINEL, device=DEV)
+    nb.embed_grad(dY, torch.from_numpy(tok).to(DEV), [[1]], G, 0, V, _ws(nb.embed_workspace_bytes(1, 1, T, V, D)))
+    rows = G.view(V, D)
+    ids = np.unique(tok[(tok >= 0) & (tok < V)])
+    want, bound = orc.embed_grad(_np(dY[0, 0]), np.where((tok[0, 0] >= 0) & (tok[0, 0] < V), np.searchsorted(ids, tok[0, 0]), -1),
+                                 len(ids), 1.0)
+    at = torch.from_numpy(ids.astype(np.int64)).to(DEV)
+    _close("G", rows[at], want, bound)
+    rows[at] = 0
+    assert int(torch.count_nonzero(rows)) == 0
+    G.normal_(generator=torch.Generator(device=DEV).manual_seed(T))
+    Y = torch.empty((1, 1, T, D), dtype=BF16, device=DEV)
+    nb.embed(G.view(1, -1), 0, V, torch.from_numpy(tok).to(DEV), [[1]], Y)
+    t = torch.from_numpy(tok[0, 0].astype(np.int64)).to(DEV)
+    inside = (t >= 0) & (t < V)
+    assert torch.equal(Y[0, 0], torch.where(inside[:, None], rows[t.clamp(0, V - 1)], 0.0).to(BF16))
+
+
+def test_the_most_mini_batches():
+    """16 learners of 64 mini-batches, half of them finished, every call."""
+    n, m, b, L, V, D, C = 16, 64, 2, 30, 11, 20, 13
+    T = b * L
+    _say("16 x 64 mini-batches")
+    rng = np.random.default_rng(4)
+    mask = (rng.random((n, m)) < 0.5).astype(np.uint8)
+    mask[0, 0], mask[n - 1, m - 1] = 0, 1
+    X = torch.from_numpy(rng.normal(size=(n, V * D + 16)).astype(np.float32)).to(DEV)
+    tok = rng.integers(-1, V + 1, (n, m, T)).astype(np.int32)
+    Y = torch.full((n, m, T, D), SENTINEL, device=DEV)
+    G = torch.full((n, m, V * D + 16), SENTINEL, device=DEV)
+    dY, _ = _rows((n, m, T, D), F32, rng=rng)
+    nb.embed(X, 0, V, torch.from_numpy(tok).to(DEV), mask, Y)
+    nb.embed_grad(dY, torch.from_numpy(tok).to(DEV), mask, G, 0, V, _ws(nb.embed_workspace_bytes(n, m, T, V, D)))
+    x, g, dh = (_rows((n, m, b, L, C), F32, rng=rng)[0].contiguous() for _ in range(3))
+    h, dx, dg = (torch.full_like(x, SENTINEL) for _ in range(3))
+    states, dh0 = torch.full((n, m, b, 1, C), SENTINEL, device=DEV), torch.full((n, m, b, C), SENTINEL, device=DEV)
+    ws = _ws(nb.scan_workspace_bytes(n, m, b, L, C))
+    nb.scan(x, g, mask, h, X=X, offset=V * D, states=states, workspace=ws)
+    nb.scan_grad(x, g, states, dh, mask, dx, dg, ws, X=X, G=G, offset=V * D, dh0=dh0)
+    packed = torch.full((n, m, nb.act_bytes(T, D)), 99, dtype=torch.uint8, device=DEV)
+    W = torch.full((n, m, D * D), SENTINEL, device=DEV)
+    nb.act_pack(Y, mask, packed)
+    nb.act_grad(packed, dY.to(BF16), mask, W, 0, D, _ws(nb.act_workspace_bytes(n, m, T, D, D)))
+    off = torch.from_numpy(mask == 0).to(DEV)
+    for t in (Y, G, h, dx, dg, states, dh0, W):
+        assert (t[off] == SENTINEL).all() and torch.isfinite(t).all()
+    assert (packed[off] == 99).all()
+    done = np.argwhere(mask)
+    for i, j in done[[0, 1, 7, len(done) // 2, -2, -1]]:
+        E, bias = _np(X[i, :V * D]).reshape(V, D), _np(X[i, V * D:V * D + C])
+        y = orc.embed(E, tok[i, j], 1.0)
+        _close("Y", Y[i, j], y, orc.U * np.abs(y))
+        want, bound = orc.embed_grad(_np(dY[i, j]), tok[i, j], V, 1.0)
+        _close("dE", G[i, j, :V * D].view(V, D), want, bound)
+        q, step = _act8(_np(Y[i, j]))
+        want, bound = orc.act_grad(q * step, _np(dY[i, j].to(BF16)))
+        _close("dW", W[i, j].view(D, D), want, bound)
+        db, edb = np.zeros(C), np.zeros(C)
+        for k in range(b):
+            args = [_np(t[i, j, k]) for t in (x, g)] + [bias, np.zeros(C), L]
+            (ho, _, _), (eh, _, _) = orc.scan(*args)
+            _close("h", h[i, j, k], ho, eh)
+            (gx, gg, g0, gb), (ex, eg, e0, egb) = orc.scan_grad(*args, _np(dh[i, j, k]), np.zeros(C))
+            _close("dx", dx[i, j, k], gx, ex)
+            _close("dg", dg[i, j, k], gg, eg)
+            _close("dh0", dh0[i, j, k], g0, e0)
+            db, edb = db + gb, edb + egb + b * orc.U * np.abs(gg).sum(0)
+        _close("dbias", G[i, j, V * D:V * D + C], db, edb)
+
+
+def test_act_grad_of_the_most_tokens():
+    """262,144 tokens, in as many parts as there may be of them."""
+    T, dim, out = 262144, 40, 9
+    _say(f"act_grad T={T}")
+    gen = torch.Generator(device=DEV).manual_seed(T)
+    A = torch.randn((1, 1, T, dim), generator=gen, device=DEV)
+    dY = torch.randn((1, 1, T, out), generator=gen, device=DEV).to(BF16)
+    packed = torch.empty((1, 1, nb.act_bytes(T, dim)), dtype=torch.uint8, device=DEV)
+    values = torch.empty_like(A)
+    nb.act_pack(A, [[1]], packed)
+    nb.act_unpack(packed, [[1]], values)
+    G = torch.empty((1, 1, dim * out), device=DEV)
+    nb.act_grad(packed, dY, [[1]], G, 0, dim, _ws(nb.act_workspace_bytes(1, 1, T, dim, out)))
+    want, bound = orc.act_grad(_np(values[0, 0]), _np(dY[0, 0]))
+    _close("G", G[0, 0].view(dim, out), want, bound)
