@@ -28,10 +28,10 @@ __device__ __forceinline__ uint32_t step_byte(float peak) {
 
 // Packing and unpacking are copies with a transposition of 32 tokens: what bounds them is HBM.
 // A thread takes V channels (8 bytes of a row in bf16, 16 in fp32) and 8 of a block's 32 tokens, four
-// threads a block; the four put their part of the peaks together by shuffles, and each has
-// 8 consecutive bytes of a channel, so that a wave writes 16 V x 32 contiguous bytes.  A
-// thread with a channel's whole block (128 bytes a load of bf16) packed at 2.3 TB/s.  It goes on
-// to the next of four blocks, whose steps make one word.
+// threads a block; the four put their parts of the peaks together by shuffles, and packing turns
+// their 4 x 4 parts of 8 bytes, so that each writes the 32 bytes of one channel and a wave 16 V x 32
+// contiguous ones.  A thread with a channel's whole block from the start (128 bytes a load of bf16)
+// packed at 2.3 TB/s, this at 4.5.  It goes on to the next of four blocks, whose steps make one word.
 template <typename T>
 struct PackTile {
   static constexpr int V = 4, CH = 16 * V;  // channels of a wave
@@ -202,8 +202,8 @@ __global__ void __launch_bounds__(256)
 // as both operands agree: of 64 tokens, octets 2 g of lanes g are step 0 and octets 2 g + 1 step 1,
 // so that
 //   A  (packed) is loaded 16 bytes a lane, 16 tokens of a channel, straight from memory, and
-//      made bf16 in registers, q * 2^k exactly; every value once, since
-//      a wave has all columns of its channels
+//      made bf16 in registers, q * 2^k exactly; every value once, since a wave has all columns
+//      of its channels
 //   B  (dY) comes a row a token: a thread turns 4 tokens x 8 columns and writes 8 bytes a
 //      column to LDS, column 8 q + e of the tile to slot e * BN / 8 + q, so that the writes and
 //      the fragment reads are contiguous and a lane's results of eight (or four) fragments are
@@ -212,12 +212,13 @@ __global__ void __launch_bounds__(256)
 // loads go out a whole stage before they are wanted.  Of eight waves, two on each SIMD (waves w
 // and w + 4), the late half runs half a stage behind: while one wave of a SIMD multiplies, the
 // other one unpacks, turns and loads, and two barriers a stage keep it so.
-// 32 mini-batches of 4096 x 1024 x 2048: 473-487 us, 1.13-1.16 PFLOP/s (a library's bf16 product of
-// 8192^3 reaches 1.17); 514 us over many passes, against 526 with both halves in step.  What
-// bounds it is power: 0.93 million cycles at 1.9 GHz, 0.52 of them the MFMAs' own, where both
-// halves in step and loads among the products took 1.21 million at 2.2 GHz.  Of the 514 us no
-// loads save 94, half the MFMAs 63, no unpacking 56, no turning 32, no LDS reads 25.  128 tokens a
-// stage, 64 channels x 256 or 128 columns a wave, two workgroups of four waves a CU took longer.
+// 32 mini-batches of 4096 x 1024 x 2048: 473 us, 1.16 PFLOP/s (a library's bf16 product of
+// 8192^3 reaches 1.17); 501-513 us over many passes, against 526 with both halves in step.  What
+// bounds it is power: 0.92 million cycles at 1.95 GHz, 0.52 of them the MFMAs' own, where both
+// halves in step and loads among the products took 1.21 million at 2.2 GHz.  Of 514 us, with an
+// unpacking of as many instructions, no loads saved 94, half the MFMAs 63, no unpacking 56, no
+// turning 32, no LDS reads 25.  128 tokens a stage, 64 channels x 256 or 128 columns a wave, two
+// workgroups of four waves a CU took longer.
 constexpr int kHB = 2, kStageTokens = kActBlock * kHB;
 template <int MT, int F, int WM, int WN>
 struct GradTile {
@@ -491,14 +492,6 @@ nbsgd_status unpack_launch(const void* packed, int32_t Tn, int32_t dim, void* A,
   return launched("nbsgd_act_unpack");
 }
 
-// Which tile a call takes: the one whose tiles cost least.  A stage of a tile takes a full card
-// 8.6 ns (256 x 256), 3.2 (128 x 128) or 1.8 (64 x 128), 475 : 175 : 100, and a card with fewer
-// tiles than `least` is not full: one large tile a CU is, one middle or small one is not.
-//   1 mini-batch of 4096 x 2048 x 2048   large 91 us, middle 73, small 60
-//   8 of 4096 x 1024 x 1024              100, 95, 116
-//   64 of 512 x 512 x 512                29, 37, 38
-//   40 of 750 x 43 x 2225                55, 43, 29
-//   64 of 2048 x 256 x 256 in two parts  48, 45, 49
 constexpr int64_t kMaxStride = 1 << 22;  // 64 rows of dY lie within 32-bit offsets
 
 // Checks shared by the two directions.
@@ -594,6 +587,14 @@ extern "C" nbsgd_status nbsgd_act_grad(const void* packed, const void* dY, int64
   c.ld = c.parts > 1 ? c.parts * size : ld;
   c.part = size;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  // Which tile a call takes: the one whose tiles cost least.  A stage of a tile takes a full card
+  // 8.6 ns (256 x 256), 3.2 (128 x 128) or 1.8 (64 x 128), 475 : 175 : 100, and a card with fewer
+  // tiles than `least` is not full: one large tile a CU is, one middle or small one is not.
+  //   1 mini-batch of 4096 x 2048 x 2048   large 89 us, middle 74, small 67
+  //   8 of 4096 x 1024 x 1024              93, 93, 111
+  //   64 of 512 x 512 x 512                29, 34, 36
+  //   40 of 750 x 43 x 2225                52, 41, 29
+  //   64 of 2048 x 256 x 256 in two parts  44, 41, 45
   const int64_t each = (int64_t)c.parts * g.count;
   const auto cost = [&](int64_t rows, int64_t columns, int64_t price, int64_t least) {
     return price * std::max(each * ceil_div(dim, rows) * ceil_div(out, columns), least);

@@ -13,10 +13,12 @@
 // alone, so it does not depend on how tiles are dealt to workgroups.  Backward, the
 // gradient mu_t = a_t (dh_t + mu_{t+1}) is the same kind of map from the last token to the
 // first; the states inside a tile are recomputed from the one kept at its start.
-// What bounds it is memory: backward, 36 mini-batches of four sequences of 2048 x 1024 bf16, 609 us
-// (3.03 GB, 4.98 TB/s; a large copy reaches 4.72); forward, 1900 x 1000 fp32 with ragged lengths,
+// What bounds it is memory: backward, 36 mini-batches of four sequences of 2048 x 1024 bf16, 614 us
+// (3.03 GB, 4.93 TB/s; a large copy reaches 4.72); forward, 1900 x 1000 fp32 with ragged lengths,
 // rows off the lines, 336 us (1.27 GB, 1.39 moved, 4.13 TB/s of them); one sequence
-// of 65536 x 2048 bf16, read twice, 265 us (1.34 GB, 5.06 TB/s).
+// of 65536 x 2048 bf16, read twice, 268 us (1.34 GB, 5.01 TB/s).  Far from it are rows narrower than
+// a wave's 128 bytes, whose other lanes idle (20 sequences of 21265 x 19 bf16: 73 us for 48 MB,
+// backward 100 for 81), and few sequences of some thousand tokens, three launches after each other.
 #include <algorithm>
 #include <type_traits>
 

@@ -109,10 +109,10 @@ NBSGD_HD int act8_sure(int tokens, int border, int c0, int width, int cols) {
 // Parts that the tokens of a weight gradient are summed in, by workgroups of their own where
 // its smallest tiles (64 x 128) are few and the tokens many.  By the mini-batch's sizes alone,
 // not by how many mini-batches a call has, so that a result does not depend on the others.
-// One mini-batch of 16384 x 1024 x 1024: 97 us in four parts, 248 in one.  A part costs a write
-// and a read of the gradient, 8 dim out bytes, so it has the tokens to read half as much again,
-// dim + 2 out bytes each: 16 mini-batches of 4096 x 1024 x 1024 take 143 us in one part and
-// 249 in four, of 8192 x 256 x 256 46 us in eight parts and 73 in two.
+// One mini-batch of 16384 x 1024 x 1024: 71 us in four parts, 96 in two, 173 in one.  A part costs a
+// write and a read of the gradient, 8 dim out bytes, so it has the tokens to read half as much again,
+// dim + 2 out bytes each: 16 mini-batches of 4096 x 1024 x 1024 take 117 us in one part and
+// 229 in four, of 8192 x 256 x 256 42 us in eight parts, 52 in two and 88 in one.
 constexpr int64_t kSplitTiles = 512, kSplitTokens = 1024;
 int act8_splits(int64_t T, int64_t dim, int64_t out);
 size_t act8_space(int64_t groups, int64_t T, int64_t dim, int64_t out);
